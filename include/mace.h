@@ -302,6 +302,63 @@ int mace_next_token_logits(mace_handle_t h, const float *y, const int32_t *row_i
 int mace_next_token_logits_static(mace_handle_t h, const float *y, const int32_t *row_idx, int32_t n, const void *g_final,
                                   const void *w_lm, float *logits_out, int32_t *next_token, void *stream);
 
+/* Embedding rows (the layer's input x of a batch of tokens; the head is tied to the same table, Section 3.1):
+ *   out[r, :] = scale * table[token_ids[r], :]
+ * table device io_dtype [vocab, d_model], token_ids device int32 [n], out device io_dtype [n, d_model] (may be x of
+ * mace_hybrid_layer_fwd).  The product is formed in fp32 and rounded once; scale = 1 copies.  A token id outside [0, vocab)
+ * stands for padding: its row of out is zero.  table and out 16-byte aligned and not overlapping; scale finite.  No workspace;
+ * one launch.  The device of mace_create must be current (MACE_INVALID_ARG otherwise; so for the three calls below). */
+int mace_embed_tokens(mace_handle_t h, const void *table, const int32_t *token_ids, int32_t n, float scale, void *out, void *stream);
+
+/* Gradient of the table behind mace_embed_tokens, e.g. from dx_ft of mace_hybrid_layer_bwd:
+ *   d_table[v, :] (+)= scale * sum over the rows r with token_ids[r] = v of dx[r, :]
+ * dx device fp32 [n, d_model], d_table device fp32 [vocab, d_model], both 16-byte aligned.  accumulate = 0: d_table is written
+ * whole, rows of tokens that do not occur become zero (also for n = 0).  accumulate != 0: added to what is there - with dw_lm of
+ * the DPO head in it, the whole gradient of a tied table - and rows of tokens that do not occur are neither read nor written.
+ * Padding (ids outside [0, vocab)) contributes nothing, whatever its rows of dx hold.  Sums are fp32, their order is a
+ * function of token_ids alone: the same call gives the same bits.  workspace: mace_embed_grad_workspace_bytes(h, n) bytes (or those of
+ * a larger n), 256-byte aligned, nothing of it read before it is written. */
+size_t mace_embed_grad_workspace_bytes(mace_handle_t h, int32_t n);
+int mace_embed_tokens_grad(mace_handle_t h, const int32_t *token_ids, int32_t n, const float *dx, float scale, float *d_table,
+                           int accumulate, void *workspace, size_t workspace_bytes, void *stream);
+
+/* Log-probabilities of given tokens from rows of logits (those of mace_next_token_logits, or any others), with the entropy and
+ * the best alternatives of every row: what a server reports beside a token, what a preference job needs of its reference
+ * policy (the per-token terms of ref_logp, Section 3.1), what a policy-gradient step weighs.
+ *   logits     device, dtype MACE_F32 or MACE_BF16, n rows of vocab columns that lie ld elements apart (ld >= vocab: the columns of a
+ *              padded head behind vocab take no part).  Aligned to its elements; rows of any alignment run at the same
+ *              rate.  vocab is the call's own (1..2^22), not the model's.
+ *   token_ids  device int32 [n], needed by logp; an id outside [0, vocab) is padding
+ *   top_k      0..32
+ * Outputs, device, each nullable (at least one, and top_ids where top_k > 0); with m = max_j x_j, L = log sum_j exp(x_j - m):
+ *   logp       fp32 [n]          x_token - m - L; 0 for padding
+ *   entropy    fp32 [n]          - sum_j p_j log p_j
+ *   row_stats  fp32 [n, 2]       m and L: the log-sum-exp is m + L, kept in two terms for logits of large magnitude
+ *   top_ids    int32 [n, top_k]  columns of the largest logits, best first, lowest column on ties; -1 behind the last token that is
+ *                                not banned
+ *   top_logp   fp32 [n, top_k]   their log-probabilities; -inf beside an id of -1
+ * A logit of -inf bans its token: probability 0, never listed.  The lowest finite value is an ordinary logit.  A row with nothing but
+ * banned tokens: logp -inf, entropy 0, row_stats (-inf, 0).  A NaN or +inf among the vocab columns of a row: its outputs are
+ * NaN (logp of padding 0) and its ids -1.  Statistics are fp32 whatever the logits' type, added in an order that depends on the sizes
+ * alone.  workspace: mace_token_logprobs_workspace_bytes(h, n, vocab, top_k) bytes, 256-byte aligned, nothing of it read before it
+ * is written. */
+size_t mace_token_logprobs_workspace_bytes(mace_handle_t h, int32_t n, int32_t vocab, int32_t top_k);
+int mace_token_logprobs(mace_handle_t h, const void *logits, int32_t dtype, int32_t n, int32_t vocab, int64_t ld,
+                        const int32_t *token_ids, int32_t top_k, float *logp, float *entropy, float *row_stats, int32_t *top_ids,
+                        float *top_logp, void *workspace, size_t workspace_bytes, void *stream);
+
+/* Gradient of the two with respect to the logits: with g = d_logp[r], h = d_entropy[r], p_j = exp(x_j - m - L),
+ *   d_logits[r, j] = g ([j = token_ids[r]] - p_j) - h p_j (log p_j + entropy[r])
+ * logits, dtype, n, vocab, ld, token_ids as above; row_stats and entropy as mace_token_logprobs wrote them for the same logits.
+ * d_logp (needs token_ids) and d_entropy (needs entropy) device fp32 [n], at least one of them.  d_logits device, d_dtype MACE_F32 or
+ * MACE_BF16 (rounded once), n rows ld_d apart, columns behind vocab left as they are; it may be logits itself (same type and
+ * stride) and overlaps nothing else.  Banned tokens have p_j = 0, so gradient 0, or g where the given token is banned.  Rows with
+ * nothing but banned tokens and rows whose two weights are 0 (padding counts as g = 0) have gradient 0, the last whatever their
+ * logits hold.  No workspace; one launch. */
+int mace_token_logprobs_grad(mace_handle_t h, const void *logits, int32_t dtype, int32_t n, int32_t vocab, int64_t ld,
+                             const int32_t *token_ids, const float *row_stats, const float *entropy, const float *d_logp,
+                             const float *d_entropy, void *d_logits, int32_t d_dtype, int64_t ld_d, void *stream);
+
 /* AdamW step (decoupled weight decay) on one tensor of n elements: the optimizer step that turns
  * the gradients of an iteration into the weights the next iteration sees (Section 2.1).  The paper
  * names no optimizer; AdamW is the reading.  step counts from 1.

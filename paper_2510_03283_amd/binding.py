@@ -21,6 +21,8 @@ EXPORTS = [
     "mace_hybrid_layer_bwd", "mace_hybrid_layer_fwd_lora", "mace_hybrid_layer_bwd_lora", "mace_dpo_logprob_loss", "mace_dpo_logprob_loss_shared",
     "mace_next_token_logits", "mace_adamw_step", "mace_head_norm_stats", "mace_kv_head_budget", "mace_profile_enable", "mace_profile_collect",
     "mace_set_option", "mace_launch_plan", "mace_next_token_logits_static", "mace_gemm_bf16",
+    "mace_embed_tokens", "mace_embed_grad_workspace_bytes", "mace_embed_tokens_grad", "mace_token_logprobs_workspace_bytes",
+    "mace_token_logprobs", "mace_token_logprobs_grad",
 ]
 MACE_OPT_HEAD_TWO_PASS, MACE_OPT_SINGLE_STREAM, MACE_OPT_DECODE_CHUNK = 1, 2, 3
 
@@ -147,6 +149,18 @@ def load():
     lib.mace_launch_plan.restype = C.c_int
     lib.mace_gemm_bf16.argtypes = [vp, C.POINTER(GemmDescT), vp]
     lib.mace_gemm_bf16.restype = C.c_int
+    lib.mace_embed_tokens.argtypes = [vp, vp, vp, i32, f32, vp, vp]
+    lib.mace_embed_tokens.restype = C.c_int
+    lib.mace_embed_grad_workspace_bytes.argtypes = [vp, i32]
+    lib.mace_embed_grad_workspace_bytes.restype = sz
+    lib.mace_embed_tokens_grad.argtypes = [vp, vp, i32, vp, f32, vp, C.c_int, vp, sz, vp]
+    lib.mace_embed_tokens_grad.restype = C.c_int
+    lib.mace_token_logprobs_workspace_bytes.argtypes = [vp, i32, i32, i32]
+    lib.mace_token_logprobs_workspace_bytes.restype = sz
+    lib.mace_token_logprobs.argtypes = [vp, vp, i32, i32, i32, i64, vp, i32, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.mace_token_logprobs.restype = C.c_int
+    lib.mace_token_logprobs_grad.argtypes = [vp, vp, i32, i32, i32, i64, vp, vp, vp, vp, vp, vp, i32, i64, vp]
+    lib.mace_token_logprobs_grad.restype = C.c_int
     _lib = lib
     return lib
 
@@ -175,10 +189,16 @@ def _stream(stream=None):
     return C.c_void_p(s.cuda_stream)
 
 
+class Handle(C.c_void_p):
+    """A mace_handle_t with what the argument checks below go by: the model, and the device that was current in mace_create."""
+
+
 def mace_create(d_model, n_q_heads, n_kv_heads, head_dim, d_ff, vocab, rms_eps, rope_theta, io_dtype):
-    h = C.c_void_p()
+    h = Handle()
     m = ModelT(d_model, n_q_heads, n_kv_heads, head_dim, d_ff, vocab, rms_eps, rope_theta, io_dtype)
     _check(load().mace_create(C.byref(h), C.byref(m)), "mace_create")
+    h.table_shape, h.io_dtype = (vocab, d_model), torch.bfloat16 if io_dtype == MACE_BF16 else torch.float32
+    h.device = torch.cuda.current_device()
     return h
 
 
@@ -348,6 +368,82 @@ def mace_next_token_logits(h, y, row_idx, n, g_final, w_lm, logits_out, next_tok
 def mace_next_token_logits_static(h, y, row_idx, n, g_final, w_lm, logits_out, next_token, stream=None):
     _check(load().mace_next_token_logits_static(h, _dev(y), _dev(row_idx), int(n), _dev(g_final), _dev(w_lm), _dev(logits_out),
                                                 _dev(next_token), _stream(stream)), "mace_next_token_logits_static")
+
+
+def _tensor(h, t, name: str, dtype, shape):
+    """Pointer of an optional tensor on the handle's device, contiguous and of this type and shape (the library is told sizes only)."""
+    if t is None:
+        return None
+    if t.get_device() != h.device or t.dtype != dtype or t.shape != shape or not t.is_contiguous():
+        raise MaceError(f"{name}: a contiguous tensor of {dtype} {tuple(shape)} on cuda:{h.device} is wanted, got {t.dtype} {tuple(t.shape)} on {t.device}")
+    return t.data_ptr()
+
+
+_IO = {torch.float32: MACE_F32, torch.bfloat16: MACE_BF16}
+
+
+def _rows(h, t, name: str, vocab):
+    """(pointer, dtype, rows, columns that count, row stride) of a matrix of logits whose columns are adjacent."""
+    if t.get_device() != h.device or t.dim() != 2 or t.dtype not in _IO or (t.stride(1) != 1 and t.shape[1] > 1):
+        raise MaceError(f"{name}: an fp32 or bf16 matrix with adjacent columns on cuda:{h.device} is wanted")
+    n, cols = t.shape
+    vocab = cols if vocab is None else int(vocab)
+    if vocab > cols:
+        raise MaceError(f"{name}: {cols} columns for a vocabulary of {vocab}")
+    return t.data_ptr(), _IO[t.dtype], n, vocab, t.stride(0) if n > 1 else cols
+
+
+def _workspace(h, t):
+    return _tensor(h, t, "workspace", t.dtype, t.shape), t.numel() * t.element_size()
+
+
+def mace_embed_tokens(h, table, token_ids, out, scale: float = 1.0, stream=None):
+    """out[r] = scale * table[token_ids[r]]; table [vocab, d_model] and out [n, d_model] in the handle's type."""
+    n = token_ids.shape[0]
+    _check(load().mace_embed_tokens(h, _tensor(h, table, "table", h.io_dtype, h.table_shape), _tensor(h, token_ids, "token_ids", torch.int32, (n,)), n, scale,
+                                    _tensor(h, out, "out", h.io_dtype, (n, h.table_shape[1])), _stream(stream)), "mace_embed_tokens")
+
+
+def mace_embed_grad_workspace_bytes(h, n: int) -> int:
+    return int(load().mace_embed_grad_workspace_bytes(h, n))
+
+
+def mace_embed_tokens_grad(h, token_ids, dx, d_table, workspace, scale: float = 1.0, accumulate=False, stream=None):
+    """d_table[v] (+)= scale * sum of dx[r] over the rows with token_ids[r] == v; dx [n, d_model], d_table [vocab, d_model] fp32."""
+    n = token_ids.shape[0]
+    _check(load().mace_embed_tokens_grad(h, _tensor(h, token_ids, "token_ids", torch.int32, (n,)), n,
+                                         _tensor(h, dx, "dx", torch.float32, (n, h.table_shape[1])), scale,
+                                         _tensor(h, d_table, "d_table", torch.float32, h.table_shape), int(accumulate), *_workspace(h, workspace),
+                                         _stream(stream)), "mace_embed_tokens_grad")
+
+
+def mace_token_logprobs_workspace_bytes(h, n: int, vocab: int, top_k: int = 0) -> int:
+    return int(load().mace_token_logprobs_workspace_bytes(h, n, vocab, top_k))
+
+
+def mace_token_logprobs(h, logits, workspace, token_ids=None, logp=None, entropy=None, row_stats=None, top_ids=None, top_logp=None, vocab=None,
+                        stream=None):
+    """Log-probability of one token a row, entropy, (max, log-sum) and top alternatives of logits [n, >= vocab] (any row stride)."""
+    p, dtype, n, vocab, ld = _rows(h, logits, "logits", vocab)
+    k = top_ids.shape[-1] if top_ids is not None else 0
+    f = torch.float32
+    _check(load().mace_token_logprobs(h, p, dtype, n, vocab, ld, _tensor(h, token_ids, "token_ids", torch.int32, (n,)), k,
+                                      _tensor(h, logp, "logp", f, (n,)), _tensor(h, entropy, "entropy", f, (n,)),
+                                      _tensor(h, row_stats, "row_stats", f, (n, 2)), _tensor(h, top_ids, "top_ids", torch.int32, (n, k)),
+                                      _tensor(h, top_logp, "top_logp", f, (n, k)), *_workspace(h, workspace), _stream(stream)), "mace_token_logprobs")
+
+
+def mace_token_logprobs_grad(h, logits, row_stats, d_logits, token_ids=None, d_logp=None, entropy=None, d_entropy=None, vocab=None, stream=None):
+    """Gradient of logp (weights d_logp) and entropy (weights d_entropy) with respect to the logits, into d_logits [n, >= vocab]."""
+    p, dtype, n, vocab, ld = _rows(h, logits, "logits", vocab)
+    q, d_dtype, n_d, _, ld_d = _rows(h, d_logits, "d_logits", vocab)
+    if n_d != n:
+        raise MaceError(f"d_logits: {n_d} rows for {n} rows of logits")
+    f = torch.float32
+    _check(load().mace_token_logprobs_grad(h, p, dtype, n, vocab, ld, _tensor(h, token_ids, "token_ids", torch.int32, (n,)),
+                                           _tensor(h, row_stats, "row_stats", f, (n, 2)), _tensor(h, entropy, "entropy", f, (n,)),
+                                           _tensor(h, d_logp, "d_logp", f, (n,)), _tensor(h, d_entropy, "d_entropy", f, (n,)), q, d_dtype, ld_d,
+                                           _stream(stream)), "mace_token_logprobs_grad")
 
 
 def mace_adamw_step(h, param, master, grad, m, v, lr, beta1, beta2, eps, weight_decay, step, stream=None):

@@ -850,6 +850,126 @@ int mace_next_token_logits_static(mace_handle_t h, const float *y, const int32_t
   return next_token_logits_impl(h, y, row_idx, n, g_final, w_lm, logits_out, next_token, h->static_scratch, STATIC_SCRATCH_BYTES, stream);
 }
 
+// The operators at the two ends of a model run on the caller's stream; like mace_next_token_logits_static they refuse a call on
+// another device than the handle's, where their pointers would belong to neither.
+static int check_device(const mace_ctx *h, const char *what) {
+  int dev = -1;
+  HIP_TRY(hipGetDevice(&dev), "hipGetDevice");
+  return dev == h->device ? MACE_OK : fail(MACE_INVALID_ARG, std::string(what) + ": the handle was created on another device than the current one");
+}
+static bool overlap(const void *a, size_t na, const void *b, size_t nb) {
+  const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
+  return x < y + nb && y < x + na;
+}
+static int check_scratch(void *workspace, size_t have, size_t need, const char *what) {
+  if (!workspace || ((uintptr_t)workspace & 255)) return fail(MACE_INVALID_ARG, std::string(what) + ": workspace must be non-null and 256-byte aligned");
+  return have >= need ? MACE_OK : fail(MACE_WORKSPACE_TOO_SMALL, std::string(what) + ": workspace too small");
+}
+
+int mace_embed_tokens(mace_handle_t h, const void *table, const int32_t *token_ids, int32_t n, float scale, void *out, void *stream) {
+  if (!h || n < 0 || (n > 0 && (!table || !token_ids || !out))) return fail(MACE_INVALID_ARG, "mace_embed_tokens: bad argument");
+  if (!std::isfinite(scale)) return fail(MACE_INVALID_ARG, "mace_embed_tokens: scale must be finite");
+  if (((uintptr_t)table | (uintptr_t)out) & 15 || (uintptr_t)token_ids & 3) return fail(MACE_INVALID_ARG, "mace_embed_tokens: table and out must be 16-byte aligned, token_ids 4-byte");
+  if (n == 0) return MACE_OK;
+  const Dims D(h->m);
+  const size_t row = (size_t)D.d * (D.bf ? 2 : 4);
+  if (overlap(out, row * n, table, row * D.V) || overlap(out, row * n, token_ids, (size_t)4 * n)) return fail(MACE_INVALID_ARG, "mace_embed_tokens: out overlaps an input");
+  TRY(check_device(h, "mace_embed_tokens"));
+  prof_mark(h, (hipStream_t)stream, T_MISC);
+  HIP_TRY(launch_embed_rows(table, D.bf, token_ids, n, D.V, D.d, scale, out, (hipStream_t)stream), "embed rows");
+  prof_mark(h, (hipStream_t)stream, -1);
+  return MACE_OK;
+}
+
+size_t mace_embed_grad_workspace_bytes(mace_handle_t h, int32_t n) {
+  if (!h || n < 0) return 0;
+  return align_up(std::max<size_t>(embed_grad_scratch_bytes(n, h->m.vocab, h->m.d_model), 1), 256);
+}
+
+int mace_embed_tokens_grad(mace_handle_t h, const int32_t *token_ids, int32_t n, const float *dx, float scale, float *d_table, int accumulate,
+                           void *workspace, size_t workspace_bytes, void *stream) {
+  if (!h || n < 0 || !d_table || (n > 0 && (!token_ids || !dx))) return fail(MACE_INVALID_ARG, "mace_embed_tokens_grad: bad argument");
+  if (!std::isfinite(scale)) return fail(MACE_INVALID_ARG, "mace_embed_tokens_grad: scale must be finite");
+  if (((uintptr_t)dx | (uintptr_t)d_table) & 15 || (uintptr_t)token_ids & 3) return fail(MACE_INVALID_ARG, "mace_embed_tokens_grad: dx and d_table must be 16-byte aligned, token_ids 4-byte");
+  const Dims D(h->m);
+  const size_t row = (size_t)D.d * 4, need = mace_embed_grad_workspace_bytes(h, n);
+  TRY(check_scratch(workspace, workspace_bytes, need, "mace_embed_tokens_grad"));
+  const struct { const void *p; size_t bytes; } in[2] = {{token_ids, (size_t)4 * n}, {dx, row * n}};
+  for (const auto &r : in)
+    if (r.bytes && (overlap(r.p, r.bytes, d_table, row * D.V) || overlap(r.p, r.bytes, workspace, need))) return fail(MACE_INVALID_ARG, "mace_embed_tokens_grad: d_table or the workspace overlaps an input");
+  if (overlap(workspace, need, d_table, row * D.V)) return fail(MACE_INVALID_ARG, "mace_embed_tokens_grad: d_table overlaps the workspace");
+  TRY(check_device(h, "mace_embed_tokens_grad"));
+  if (n == 0 && accumulate) return MACE_OK;
+  prof_mark(h, (hipStream_t)stream, T_MISC);
+  HIP_TRY(launch_embed_grad(token_ids, n, D.V, D.d, dx, scale, d_table, accumulate != 0, workspace, (hipStream_t)stream), "embed grad");
+  prof_mark(h, (hipStream_t)stream, -1);
+  return MACE_OK;
+}
+
+static int check_logits(const void *p, int32_t dtype, int32_t n, int32_t vocab, int64_t ld, const char *what) {
+  if (n < 0 || (n > 0 && !p)) return fail(MACE_INVALID_ARG, std::string(what) + ": bad argument");
+  if (dtype != MACE_F32 && dtype != MACE_BF16) return fail(MACE_INVALID_ARG, std::string(what) + ": dtype must be MACE_F32 or MACE_BF16");
+  if (vocab <= 0 || vocab > LOGPROBS_MAX_VOCAB) return fail(MACE_BAD_SHAPE, std::string(what) + ": vocab must be in 1..2^22");
+  if (ld < vocab || ld > INT32_MAX) return fail(MACE_BAD_SHAPE, std::string(what) + ": the row stride must be at least vocab and below 2^31");
+  if ((uintptr_t)p & (dtype == MACE_BF16 ? 1 : 3)) return fail(MACE_INVALID_ARG, std::string(what) + ": pointer not aligned to its elements");
+  return MACE_OK;
+}
+// Bytes from the first to the last element of rows that lie ld apart.
+static size_t rows_bytes(int32_t n, int32_t vocab, int64_t ld, int32_t dtype) {
+  return n ? ((size_t)(n - 1) * (size_t)ld + (size_t)vocab) * (dtype == MACE_BF16 ? 2 : 4) : 0;
+}
+
+size_t mace_token_logprobs_workspace_bytes(mace_handle_t h, int32_t n, int32_t vocab, int32_t top_k) {
+  if (!h || n < 0 || vocab <= 0 || vocab > LOGPROBS_MAX_VOCAB || top_k < 0 || top_k > TOP_K_MAX) return 0;
+  return align_up(std::max<size_t>(token_logprobs_scratch_bytes(n, vocab, top_k), 1), 256);
+}
+
+int mace_token_logprobs(mace_handle_t h, const void *logits, int32_t dtype, int32_t n, int32_t vocab, int64_t ld, const int32_t *token_ids,
+                        int32_t top_k, float *logp, float *entropy, float *row_stats, int32_t *top_ids, float *top_logp, void *workspace,
+                        size_t workspace_bytes, void *stream) {
+  const char *what = "mace_token_logprobs";
+  if (!h) return fail(MACE_INVALID_ARG, "handle is null");
+  TRY(check_logits(logits, dtype, n, vocab, ld, what));
+  if (top_k < 0 || top_k > TOP_K_MAX) return fail(MACE_BAD_SHAPE, "mace_token_logprobs: top_k must be in 0..32");
+  if (n == 0) return MACE_OK;
+  if (!logp && !entropy && !row_stats && !top_k) return fail(MACE_INVALID_ARG, "mace_token_logprobs: no output is asked for");
+  if (logp && !token_ids) return fail(MACE_INVALID_ARG, "mace_token_logprobs: logp needs token_ids");
+  if (top_k > 0 ? !top_ids : top_ids || top_logp) return fail(MACE_INVALID_ARG, "mace_token_logprobs: top_k needs top_ids, and top_ids or top_logp need top_k");
+  if (((uintptr_t)token_ids | (uintptr_t)logp | (uintptr_t)entropy | (uintptr_t)row_stats | (uintptr_t)top_ids | (uintptr_t)top_logp) & 3) return fail(MACE_INVALID_ARG, "mace_token_logprobs: pointer not aligned to its elements");
+  TRY(check_scratch(workspace, workspace_bytes, mace_token_logprobs_workspace_bytes(h, n, vocab, top_k), what));
+  TRY(check_device(h, what));
+  const TokenLogprobs a = {logits, ld, n, vocab, top_k, token_ids, logp, entropy, row_stats, top_logp, top_ids};
+  prof_mark(h, (hipStream_t)stream, T_LOGSOFTMAX);
+  HIP_TRY(launch_token_logprobs(a, dtype == MACE_BF16, workspace, (hipStream_t)stream), "token logprobs");
+  prof_mark(h, (hipStream_t)stream, -1);
+  return MACE_OK;
+}
+
+int mace_token_logprobs_grad(mace_handle_t h, const void *logits, int32_t dtype, int32_t n, int32_t vocab, int64_t ld, const int32_t *token_ids,
+                             const float *row_stats, const float *entropy, const float *d_logp, const float *d_entropy, void *d_logits,
+                             int32_t d_dtype, int64_t ld_d, void *stream) {
+  const char *what = "mace_token_logprobs_grad";
+  if (!h) return fail(MACE_INVALID_ARG, "handle is null");
+  TRY(check_logits(logits, dtype, n, vocab, ld, what));
+  TRY(check_logits(d_logits, d_dtype, n, vocab, ld_d, what));
+  if (n == 0) return MACE_OK;
+  if (!row_stats || (!d_logp && !d_entropy)) return fail(MACE_INVALID_ARG, "mace_token_logprobs_grad: row_stats and d_logp or d_entropy are needed");
+  if (d_logp && !token_ids) return fail(MACE_INVALID_ARG, "mace_token_logprobs_grad: d_logp needs token_ids");
+  if (d_entropy && !entropy) return fail(MACE_INVALID_ARG, "mace_token_logprobs_grad: d_entropy needs the rows' entropy");
+  if (((uintptr_t)token_ids | (uintptr_t)row_stats | (uintptr_t)entropy | (uintptr_t)d_logp | (uintptr_t)d_entropy) & 3) return fail(MACE_INVALID_ARG, "mace_token_logprobs_grad: pointer not aligned to its elements");
+  const bool in_place = logits == d_logits && dtype == d_dtype && ld == ld_d;
+  const size_t out = rows_bytes(n, vocab, ld_d, d_dtype);
+  if (!in_place && overlap(logits, rows_bytes(n, vocab, ld, dtype), d_logits, out)) return fail(MACE_INVALID_ARG, "mace_token_logprobs_grad: d_logits overlaps logits without being the same rows");
+  for (const void *p : {(const void *)token_ids, (const void *)row_stats, (const void *)entropy, (const void *)d_logp, (const void *)d_entropy})
+    if (p && overlap(p, (size_t)(p == row_stats ? 8 : 4) * n, d_logits, out)) return fail(MACE_INVALID_ARG, "mace_token_logprobs_grad: d_logits overlaps an input");
+  TRY(check_device(h, what));
+  const TokenLogprobsGrad a = {logits, ld, ld_d, n, vocab, row_stats, entropy, d_logp, d_entropy, token_ids, d_logits};
+  prof_mark(h, (hipStream_t)stream, T_DLOGITS);
+  HIP_TRY(launch_token_logprobs_grad(a, dtype == MACE_BF16, d_dtype == MACE_BF16, (hipStream_t)stream), "token logprobs gradient");
+  prof_mark(h, (hipStream_t)stream, -1);
+  return MACE_OK;
+}
+
 int mace_adamw_step(mace_handle_t h, void *param, float *master, const float *grad, float *m, float *v, int64_t n, float lr,
                     float beta1, float beta2, float eps, float weight_decay, int32_t step, void *stream) {
   if (!h || !param || !grad || !m || !v || n < 0) return fail(MACE_INVALID_ARG, "mace_adamw_step: bad argument");

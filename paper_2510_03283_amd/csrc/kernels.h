@@ -236,3 +236,37 @@ hipError_t launch_scale_rows(float *u, const bf16_t *n_hi, bf16_t *n_c, const in
 hipError_t launch_dpo_pairs(const float *logp_t, const int32_t *ft_seq_offsets, const int32_t *prompt_lens, int n_seq,
                             int rows, const float *ref_logp, float beta, float *logp_out, float *loss_per_pair, float *loss_mean,
                             float *clpd, int32_t *win, float *dlogp, hipStream_t st);
+
+// ---- embed.hip -------------------------------------------------------------------------------
+// out[r, :] = scale * table[ids[r], :] in the table's type (fp32 or bf16); zeros where ids[r] is outside [0, vocab).  d % 64 == 0.
+hipError_t launch_embed_rows(const void *table, bool bf16, const int32_t *ids, int n, int vocab, int d, float scale, void *out, hipStream_t st);
+// d_table[v, :] = scale * sum of dx[r, :] over the rows with ids[r] == v, in an order that the ids alone decide; added to what is there
+// when accumulate, in which case rows of tokens that do not occur are not touched.  scratch: embed_grad_scratch_bytes, 256-byte aligned.
+size_t embed_grad_scratch_bytes(int n, int vocab, int d);
+hipError_t launch_embed_grad(const int32_t *ids, int n, int vocab, int d, const float *dx, float scale, float *d_table, bool accumulate,
+                             void *scratch, hipStream_t st);
+
+// ---- token_logprobs.hip ----------------------------------------------------------------------
+constexpr int TOP_K_MAX = 32;
+constexpr int LOGPROBS_MAX_VOCAB = 1 << 22;
+// Rows of logits [n, vocab] (row stride ld) -> outputs, each nullable; see mace_token_logprobs.
+struct TokenLogprobs {
+  const void *logits;
+  long long ld;
+  int n, vocab, top_k;
+  const int32_t *token_ids;
+  float *logp, *entropy, *row_stats, *top_logp;
+  int32_t *top_ids;
+};
+size_t token_logprobs_scratch_bytes(int n, int vocab, int top_k);
+hipError_t launch_token_logprobs(const TokenLogprobs &a, bool bf16, void *scratch, hipStream_t st);
+// d_logits [n, vocab] (row stride ld_d); d_logp (with token_ids) or d_entropy (with entropy) may be null; see mace_token_logprobs_grad.
+struct TokenLogprobsGrad {
+  const void *logits;
+  long long ld, ld_d;
+  int n, vocab;
+  const float *row_stats, *entropy, *d_logp, *d_entropy;
+  const int32_t *token_ids;
+  void *d_logits;
+};
+hipError_t launch_token_logprobs_grad(const TokenLogprobsGrad &a, bool bf16, bool out_bf16, hipStream_t st);

@@ -119,6 +119,7 @@ class DeviceIteration:
         self.dh = torch.empty((self.Tf, m.d_model), **f32)
         self.dE = torch.empty((m.vocab, m.d_model), **f32)
         self.dgf = torch.empty(m.d_model, **f32)
+        self.embed_ws = None                     # scratch of embed_grad, made when it is first called
         self.dx = torch.empty((self.Tf, m.d_model), **f32)
         self.grads = {k: torch.empty(self.w[k].shape, **f32) for k in _WNAMES}
         self.g_struct = B.layer_grads_struct(self.grads)
@@ -160,6 +161,17 @@ class DeviceIteration:
         k = torch.from_numpy(np.concatenate(ks).astype(np.float32)).to(self.dev).to(self.io_dtype).contiguous()
         v = torch.from_numpy(np.concatenate(vs).astype(np.float32)).to(self.dev).to(self.io_dtype).contiguous()
         B.mace_kv_cache_append(self.h, self.cache, k, v, sl, int(sl.numel()))
+
+    def embed(self, token_ids, scale: float = 1.0):
+        """The layer's input from the ids of all rows (device int32 [T]) through mace_embed_tokens."""
+        B.mace_embed_tokens(self.h, self.E, token_ids, self.x, scale)
+
+    def embed_grad(self, token_ids_ft, scale: float = 1.0):
+        """Adds the lookup's part of the tied table's gradient to dE, where dpo() left the head's: after backward()."""
+        n = B.mace_embed_grad_workspace_bytes(self.h, self.Tf)
+        if self.embed_ws is None or self.embed_ws.numel() < n:
+            self.embed_ws = torch.empty(n, dtype=torch.uint8, device=self.dev)
+        B.mace_embed_tokens_grad(self.h, token_ids_ft, self.dx, self.dE, self.embed_ws, scale, accumulate=True)
 
     def forward(self):
         if self.lora is not None:

@@ -1,0 +1,94 @@
+"""Host side of the operators at the two ends of a model, on a machine without a GPU: what they refuse (before anything is
+launched) and what they launch (token_ops_recorder.cpp)."""
+import json
+import os
+import subprocess
+
+import pytest
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+OK, INVALID, SHAPE, SMALL = 0, -1, -2, -3
+
+
+@pytest.fixture(scope="module")
+def recorder(tmp_path_factory):
+    from paper_2510_03283_amd import build
+    objs = [os.path.join(build.BUILD_DIR, s[:-4] + ".o") for s in build.sources()]
+    if not all(os.path.exists(o) for o in objs):
+        build.build_library()
+    d = tmp_path_factory.mktemp("token_ops")
+    obj, exe = str(d / "recorder.o"), str(d / "recorder")
+    subprocess.run([build.HIPCC, "-x", "hip", "--offload-host-only", "-fPIE", "-std=c++17", "-O1", "-I", build.CSRC, "-c",
+                    os.path.join(ROOT, "tests", "token_ops_recorder.cpp"), "-o", obj], check=True)
+    subprocess.run(["g++", obj, *objs, "-o", exe], check=True)
+
+    def run(call, **opts):
+        out = subprocess.run([exe, call, *(f"{k}={v}" for k, v in opts.items())], capture_output=True, text=True, check=True).stdout
+        rec = [json.loads(l) for l in out.splitlines()]
+        end = rec[-1]
+        return end["status"], end["error"], [r for r in rec if r["op"] == "launch"], next(r["bytes"] for r in rec if r["op"] == "need")
+
+    return run
+
+
+REFUSED = [
+    ("embed", dict(null="handle"), INVALID), ("embed", dict(null="table"), INVALID), ("embed", dict(null="ids"), INVALID), ("embed", dict(null="out"), INVALID),
+    ("embed", dict(n=-1), INVALID), ("embed", dict(scale="nan"), INVALID), ("embed", dict(scale="inf"), INVALID),
+    ("embed", dict(misalign="table", by=8), INVALID), ("embed", dict(misalign="out", by=8), INVALID), ("embed", dict(misalign="ids", by=2), INVALID),
+    ("embed", dict(same="table,out"), INVALID), ("embed", dict(same="table,out", offset=1048560), INVALID), ("embed", dict(device=1), INVALID),
+    ("embed_grad", dict(null="handle"), INVALID), ("embed_grad", dict(null="ids"), INVALID), ("embed_grad", dict(null="dx"), INVALID),
+    ("embed_grad", dict(null="d_table"), INVALID), ("embed_grad", dict(null="work"), INVALID), ("embed_grad", dict(n=-3), INVALID),
+    ("embed_grad", dict(scale="nan"), INVALID), ("embed_grad", dict(misalign="dx", by=4), INVALID), ("embed_grad", dict(misalign="d_table", by=4), INVALID),
+    ("embed_grad", dict(misalign="work", by=16), INVALID), ("embed_grad", dict(work=0), SMALL), ("embed_grad", dict(same="dx,d_table"), INVALID),
+    ("embed_grad", dict(same="dx,work"), INVALID), ("embed_grad", dict(same="d_table,work"), INVALID), ("embed_grad", dict(device=1), INVALID),
+    ("logprobs", dict(null="handle"), INVALID), ("logprobs", dict(null="logits"), INVALID), ("logprobs", dict(null="ids"), INVALID),
+    ("logprobs", dict(null="work"), INVALID), ("logprobs", dict(no_outputs=1), INVALID), ("logprobs", dict(n=-1), INVALID), ("logprobs", dict(dtype=2), INVALID),
+    ("logprobs", dict(vocab=0), SHAPE), ("logprobs", dict(vocab=(1 << 22) + 1), SHAPE), ("logprobs", dict(vocab=100, ld=99), SHAPE),
+    ("logprobs", dict(ld=1 << 31), SHAPE), ("logprobs", dict(top_k=33), SHAPE), ("logprobs", dict(top_k=-1), SHAPE),
+    ("logprobs", dict(top_k=5, null="top_ids"), INVALID), ("logprobs", dict(top_k=0, top=1), INVALID), ("logprobs", dict(misalign="logits"), INVALID),
+    ("logprobs", dict(misalign="logits", by=1, dtype=1), INVALID), ("logprobs", dict(misalign="logp"), INVALID), ("logprobs", dict(misalign="work", by=64), INVALID),
+    ("logprobs", dict(work=0), SMALL), ("logprobs", dict(n=1, vocab=32000, top_k=5, work=0), SMALL), ("logprobs", dict(device=1), INVALID),
+    ("logprobs_grad", dict(null="handle"), INVALID), ("logprobs_grad", dict(null="logits"), INVALID), ("logprobs_grad", dict(null="stats"), INVALID),
+    ("logprobs_grad", dict(null="ids"), INVALID), ("logprobs_grad", dict(null="entropy"), INVALID), ("logprobs_grad", dict(null="d_logits"), INVALID),
+    ("logprobs_grad", dict(no_weights=1), INVALID), ("logprobs_grad", dict(d_dtype=7), INVALID), ("logprobs_grad", dict(vocab=9, ld_d=8), SHAPE),
+    ("logprobs_grad", dict(same="logits,d_logits", d_dtype=1), INVALID),                       # bf16 over fp32 rows
+    ("logprobs_grad", dict(same="logits,d_logits", d_dtype=0, ld_d=2056), INVALID),            # another stride
+    ("logprobs_grad", dict(same="logits,d_logits", d_dtype=0, offset=4), INVALID),             # the same rows, one element on
+    ("logprobs_grad", dict(same="stats,d_logits", d_dtype=0), INVALID), ("logprobs_grad", dict(misalign="d_logits", by=1), INVALID),
+    ("logprobs_grad", dict(device=1), INVALID),
+]
+
+
+@pytest.mark.parametrize("call,opts,status", REFUSED, ids=[f"{c}-{'-'.join(f'{k}={v}' for k, v in o.items())}" for c, o, _ in REFUSED])
+def test_refused_before_anything_is_launched(recorder, call, opts, status):
+    got, error, launches, _ = recorder(call, **opts)
+    assert got == status and error and not launches
+
+
+@pytest.mark.parametrize("call", ["embed", "embed_grad", "logprobs", "logprobs_grad"])
+def test_good_calls_launch_on_the_callers_stream(recorder, call):
+    for opts in (dict(), dict(n=1), dict(n=70000)):
+        got, error, launches, _ = recorder(call, **opts)
+        assert got == OK, error
+        assert launches and all(l["stream"] == 0 and l["block"] <= 1024 for l in launches)
+        assert all(l["grid"][0] * l["block"] < 1 << 32 and l["grid"][1] < 1 << 16 and l["grid"][2] < 1 << 16 for l in launches)
+
+
+def test_no_rows(recorder):
+    for call in ("embed", "logprobs", "logprobs_grad"):
+        assert recorder(call, n=0)[:3] == (OK, "", [])
+    assert recorder("embed_grad", n=0, accumulate=1)[:3] == (OK, "", [])
+    assert recorder("embed_grad", n=0, accumulate=0)[2]               # the table is still cleared
+
+
+def test_gradient_over_its_own_logits(recorder):
+    assert recorder("logprobs_grad", same="logits,d_logits", d_dtype=0)[0] == OK
+    assert recorder("logprobs_grad", same="logits,d_logits", dtype=1, d_dtype=1, ld=2056, ld_d=2056)[0] == OK
+
+
+def test_workspace_of_more_rows_serves_fewer(recorder):
+    sizes = [1, 2, 3, 31, 64, 65, 100, 255, 256, 257, 511, 513, 1000, 4095, 4096, 4097, 16384, 20001, 65536, 100000]
+    need = [recorder("embed_grad", n=n)[3] for n in sizes]
+    assert need == sorted(need)
+    for vocab, k in ((100, 0), (2048, 5), (32000, 0), (32000, 20), (128011, 32), (1 << 22, 1)):
+        assert all(recorder("logprobs", n=n, vocab=vocab, top_k=k)[3] >= 256 for n in (1, 7, 300, 5000))
