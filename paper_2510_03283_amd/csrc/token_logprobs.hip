@@ -12,8 +12,11 @@
 
 namespace {
 
-constexpr float LOWEST = -3.402823466e38f, LOG2E = 1.44269504088896340736f;
-constexpr float FAR = -1e4f;            // differences of logits below this have e^x = 0; clamped, 0 times one is 0 and not NaN
+constexpr float LOWEST = -3.402823466e38f, LOG2E = 1.44269504088896340736f, LN2 = 0.693147180559945309417f;
+// Differences of logits (in units of log 2: FAR2) below these have an exponential of 0; clamped, 0 times one is 0 and not NaN.
+constexpr float FAR = -1e4f, FAR2 = -1.4e4f;
+// Up to this magnitude of a row's maximum the rounding of its product with log2 e is a small part of an exponent (at most 0.06).
+constexpr float BIG = 1e6f;
 
 // 16 bytes of a row: 4 fp32 or 8 bf16 values.  Rows start at any element (odd vocabularies, padded heads), and a 16-byte access needs
 // no more than its elements' alignment: a wave's 1 KB then touches one cache line more.
@@ -48,168 +51,221 @@ struct Chunk {
   }
 };
 
+// The reference of a thread's terms: its maximum in units of log 2, ROUNDED - as a product that is never contracted into what uses it.
+__device__ __forceinline__ float reference_of(float m) {
+#pragma clang fp contract(off)
+  return fmaxf(m, -BIG) * LOG2E;
+}
 __device__ __forceinline__ float exp_of(float t) { return __builtin_amdgcn_exp2f(t * LOG2E); }
-__device__ __forceinline__ bool better(float v, int i, float w, int j) { return v > w || (v == w && i < j); }
+
+// Reductions over a wave without LDS: quads, halves and rows of 16 lanes by DPP, the four rows through scalar registers.
+template <int CTRL>
+__device__ __forceinline__ float dpp(float x) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, 0xf, 0xf, true));
+}
+constexpr int QUAD_XOR_1 = 0xB1, QUAD_XOR_2 = 0x4E, HALF_MIRROR = 0x141, MIRROR = 0x140;
+__device__ __forceinline__ float lane_of(float x, int lane) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), lane)); }
+__device__ __forceinline__ float max_quad(float x) {
+  x = fmaxf(x, dpp<QUAD_XOR_1>(x));
+  return fmaxf(x, dpp<QUAD_XOR_2>(x));
+}
+__device__ __forceinline__ float max_row16(float x) {
+  x = max_quad(x);
+  x = fmaxf(x, dpp<HALF_MIRROR>(x));
+  return fmaxf(x, dpp<MIRROR>(x));
+}
+__device__ __forceinline__ float max_all(float x) {
+  x = max_row16(x);
+  return fmaxf(fmaxf(lane_of(x, 0), lane_of(x, 16)), fmaxf(lane_of(x, 32), lane_of(x, 48)));
+}
+__device__ __forceinline__ float sum_all(float x) {
+  x += dpp<QUAD_XOR_1>(x);
+  x += dpp<QUAD_XOR_2>(x);
+  x += dpp<HALF_MIRROR>(x);
+  x += dpp<MIRROR>(x);
+  return (lane_of(x, 0) + lane_of(x, 16)) + (lane_of(x, 32) + lane_of(x, 48));
+}
 
 // What a set of columns contributes: ones + rest = sum e^(x - m), u = sum (x - m) e^(x - m).  `ones` counts columns that hold the
-// maximum (at least one of each thread that met it; others are in rest), so that the logarithm of a sum just above 1 keeps its digits.
+// maximum (one of each thread that met it; others are in rest), so that the logarithm of a sum just above 1 keeps its digits.
 struct State {
   float m, ones, rest, u;
 };
-template <int NT>
-__device__ __forceinline__ float3 block_sum3(float3 v, float (*red)[3]) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) {
-    v.x += __shfl_xor(v.x, o, 64);
-    v.y += __shfl_xor(v.y, o, 64);
-    v.z += __shfl_xor(v.z, o, 64);
-  }
-  const int w = threadIdx.x >> 6;
-  if ((threadIdx.x & 63) == 0) { red[w][0] = v.x; red[w][1] = v.y; red[w][2] = v.z; }
-  __syncthreads();
-  float3 t = make_float3(red[0][0], red[0][1], red[0][2]);
-#pragma unroll
-  for (int i = 1; i < NT / 64; ++i) { t.x += red[i][0]; t.y += red[i][1]; t.z += red[i][2]; }
-  return t;
+
+// log(1 + y), y >= 0, to about 2 ulp also where it is small: 2 artanh(y / (2 + y)) up to y = 0.5, where the first term left out is 4e-9.
+__device__ __forceinline__ float log_1p(float y) {
+  const float t = y * __builtin_amdgcn_rcpf(2.f + y), z = t * t;
+  const float small = 2.f * fmaf(t * z, fmaf(z, fmaf(z, fmaf(z, 1.f / 9.f, 1.f / 7.f), 1.f / 5.f), 1.f / 3.f), t);
+  return y <= 0.5f ? small : __builtin_amdgcn_logf(1.f + y) * LN2;
 }
 
 struct Row {
   float m, L;          // statistics as they are reported
-  bool empty, bad;
+  int empty, bad;
   __device__ __forceinline__ float logp(float x) const { return bad ? NAN : empty ? -INFINITY : x - m - L; }
 };
-__device__ __forceinline__ Row finish(const State &t, const TokenLogprobs &a, size_t r, float x_token, bool writes) {
+__device__ __forceinline__ Row finish(const State &t, const TokenLogprobs &a, size_t r, bool given, float x_token, bool writes) {
   Row o;
   const float s = t.ones + t.rest;
   o.bad = s != s;
   o.empty = s == 0.f;
   o.m = o.bad ? NAN : o.empty ? -INFINITY : t.m;
-  o.L = o.bad ? NAN : o.empty ? 0.f : log1pf((t.ones - 1.f) + t.rest);
+  o.L = o.bad ? NAN : o.empty ? 0.f : log_1p((t.ones - 1.f) + t.rest);
   if (writes) {
     if (a.row_stats) {
       a.row_stats[2 * r] = o.m;
       a.row_stats[2 * r + 1] = o.L;
     }
-    if (a.entropy) a.entropy[r] = o.empty ? 0.f : o.L - t.u / s;
-    if (a.logp) {
-      const int tok = a.token_ids[r];
-      a.logp[r] = tok >= 0 && tok < a.vocab ? o.logp(x_token) : 0.f;
-    }
+    if (a.entropy) a.entropy[r] = o.empty ? 0.f : o.L - t.u * __builtin_amdgcn_rcpf(s);
+    if (a.logp) a.logp[r] = given ? o.logp(x_token) : 0.f;
   }
   return o;
 }
 
-constexpr int NT = 256, U = 4;                   // threads of a block; 16-byte accesses of a thread in a turn
-constexpr int MAX_TURNS = 32;                    // turns of a part (LDS: 64 group maxima each)
+constexpr int NT = 256, WAVES = NT / 64;         // threads and waves of a block
+constexpr int U = 4;                             // 16-byte accesses of a thread in a turn
+constexpr int MAX_GROUPS = 2048;                 // group maxima that LDS holds: 131072 fp32 columns of a part
 constexpr int CAND = 1024;                       // candidates for the alternatives that LDS holds
+constexpr int RANK_STEP = 8;
 
-// Columns [c0, c1) of a row.  A turn is NT * U consecutive 16-byte accesses; the four lanes of a quad hold U x 64 bytes of it, a
-// group, whose maximum is kept: the alternatives are then found without a second pass over the row.
+// A turn is NT * U consecutive 16-byte accesses; the four lanes of a quad hold U x 64 bytes of it, a group, whose maximum is
+// kept: the alternatives are then found without a second pass over the row.
 template <bool BF16>
 struct Turn {
-  static constexpr int N = Chunk<BF16>::N, COLS = NT * U * N, GROUPS = NT / 4, GROUP_COLS = 4 * U * N;
+  static constexpr int N = Chunk<BF16>::N, COLS = NT * U * N, GROUPS = NT / 4, GROUP_COLS = 4 * U * N, MAX_TURNS = MAX_GROUPS / GROUPS;
   static __device__ __forceinline__ int column(int turn, int u, int thread) { return turn * COLS + (u * NT + thread) * N; }
 };
 
+// A column that may be among the best, as one number that is larger for the better one: the logit's bits, made monotonic, over the
+// complement of the column (equal logits: the lower column).  -0 counts as 0.
+typedef unsigned long long Candidate;
+__device__ __forceinline__ Candidate candidate(float v, int col) {
+  const uint32_t b = __float_as_uint(v + 0.f);
+  return (Candidate)(b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u)) << 32 | (uint32_t)~col;
+}
+__device__ __forceinline__ float value_of(Candidate c) {
+  const uint32_t b = (uint32_t)(c >> 32);
+  return __uint_as_float(b & 0x80000000u ? b ^ 0x80000000u : ~b);
+}
+__device__ __forceinline__ int column_of(Candidate c) { return (int)~(uint32_t)c; }
 struct TopScratch {
-  float group[MAX_TURNS * NT / 4];
-  float quad[64];
-  float v[CAND];
-  int id[CAND];
-  int list[MAX_TURNS * NT / 4];
-  int n_list, n_cand, scan[4];
+  alignas(16) Candidate c[CAND + RANK_STEP];
+  float group[MAX_GROUPS];
+  uint16_t list[MAX_GROUPS];
+  alignas(16) float set[64];
+  int n_list, n_cand, scan[WAVES];
   float tau;
+  Row row;
 };
 
-// Appends the columns of the listed groups whose value passes (strict ? > : >=) tau; a wave reads eight groups at a time.
-template <bool BF16>
-__device__ void collect(TopScratch &S, const void *row, int c0, int c1, float tau, bool strict) {
-  using T = Turn<BF16>;
-  constexpr int PER = T::GROUP_COLS / 64;        // values of a lane and group
-  const int lane = threadIdx.x & 63, n = S.n_list;
-  for (int i0 = (threadIdx.x >> 6) * 8; i0 < n; i0 += 32) {
-    float x[8 * PER];
-    int col[8 * PER];
+// Appends the passing lanes' items to a list in LDS whose length is *n: one atomic a wave; the order of the items is not used.
+template <typename T>
+__device__ __forceinline__ void append(T *list, int most, int *n, bool pass, T item) {
+  const unsigned long long b = __ballot(pass);
+  if (!b) return;
+  int at = 0;
+  if ((threadIdx.x & 63) == 0) at = atomicAdd(n, __popcll(b));
+  at = __builtin_amdgcn_readfirstlane(at) + __popcll(b & ((1ull << (threadIdx.x & 63)) - 1));
+  if (pass && at < most) list[at] = item;
+}
+
+// The k-th largest of 64 values (LOWEST where there is none), one in every lane; k <= 64.
+__device__ __forceinline__ float kth_of_64(const float *set, int k) {
+  const float v = set[threadIdx.x & 63];
+  int above = 0;
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      const int g = S.list[min(i0 + k, n - 1)];
+  for (int j = 0; j < 64; j += 32) {
+    float4 w[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) w[i] = *(const float4 *)(set + j + 4 * i);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) above += (w[i].x > v) + (w[i].y > v) + (w[i].z > v) + (w[i].w > v);
+  }
+  return -max_all(above < k ? -v : -INFINITY);   // the least of those with fewer than k above them
+}
+
+// Leaves the columns whose value passes (strict ? > : >=) tau in S.c and returns their number, of which S.c holds CAND: lists the
+// groups whose maximum passes, and reads those again, eight loads of a wave at a time.
+template <bool BF16>
+__device__ __forceinline__ int collect(TopScratch &S, const void *row, int c0, int c1, int n_groups, float tau, bool strict) {
+  using T = Turn<BF16>;
+  constexpr int PER = T::GROUP_COLS / 64, AT_ONCE = 8 / PER;    // adjacent columns of a lane and group; groups
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  for (int g = threadIdx.x; g < n_groups; g += NT) {            // n_groups is a multiple of 64
+    const float v = S.group[g];
+    append(S.list, MAX_GROUPS, &S.n_list, strict ? v > tau : v >= tau, (uint16_t)g);
+  }
+  __syncthreads();
+  const int n = S.n_list;
+  const int in_group = T::column(0, lane / 16, 0) + lane % 16 * PER;       // a group: U runs of 64 bytes
+  for (int i0 = wave; i0 < n; i0 += WAVES * AT_ONCE) {
+    float x[AT_ONCE][PER];
+    int first[AT_ONCE];
+#pragma unroll
+    for (int k = 0; k < AT_ONCE; ++k) {
+      if (i0 + k * WAVES >= n) break;
+      const int g = __builtin_amdgcn_readfirstlane((int)S.list[i0 + k * WAVES]);
+      first[k] = c0 + T::column(g / T::GROUPS, 0, 4 * (g % T::GROUPS));
+#pragma unroll
+      for (int e = 0; e < PER; ++e) x[k][e] = ld_io<BF16>(row, first[k] + min(in_group + e, c1 - 1 - first[k]));
+    }
+    unsigned long long pass[AT_ONCE][PER];
+    int total = 0, at = 0;
+#pragma unroll
+    for (int k = 0; k < AT_ONCE; ++k) {
+      if (i0 + k * WAVES >= n) break;
 #pragma unroll
       for (int e = 0; e < PER; ++e) {
-        const int at = lane + 64 * e, u = at / (4 * T::N), in = at % (4 * T::N);
-        const int c = c0 + T::column(g / T::GROUPS, u, 4 * (g % T::GROUPS)) + in;
-        col[k * PER + e] = i0 + k < n && c < c1 ? c : -1;
-        x[k * PER + e] = ld_io<BF16>(row, min(c, c1 - 1));
+        pass[k][e] = __ballot(in_group + e < c1 - first[k] && (strict ? x[k][e] > tau : x[k][e] >= tau));
+        total += __popcll(pass[k][e]);
       }
     }
+    if (!total) continue;
+    if (lane == 0) at = atomicAdd(&S.n_cand, total);
+    at = __builtin_amdgcn_readfirstlane(at);
 #pragma unroll
-    for (int k = 0; k < 8 * PER; ++k)
-      if (col[k] >= 0 && (strict ? x[k] > tau : x[k] >= tau)) {
-        const int at = atomicAdd(&S.n_cand, 1);
-        if (at < CAND) { S.v[at] = x[k]; S.id[at] = col[k]; }
+    for (int k = 0; k < AT_ONCE; ++k) {
+      if (i0 + k * WAVES >= n) break;
+#pragma unroll
+      for (int e = 0; e < PER; ++e) {
+        const int mine = at + __popcll(pass[k][e] & ((1ull << lane) - 1));
+        if (((pass[k][e] >> lane) & 1) && mine < CAND) S.c[mine] = candidate(x[k][e], first[k] + in_group + e);
+        at += __popcll(pass[k][e]);
       }
+    }
   }
+  __syncthreads();
+  return S.n_cand;
 }
 
-__device__ __forceinline__ void list_groups(TopScratch &S, int n_groups, float tau, bool strict) {
-  for (int i = threadIdx.x; i < n_groups; i += NT)
-    if (strict ? S.group[i] > tau : S.group[i] >= tau) S.list[atomicAdd(&S.n_list, 1)] = i;
-}
-
-__device__ __forceinline__ int rank_of(const TopScratch &S, int i, int n) {
+// How many of list[0 .. n) are better than c.  RANK_STEP at a time: the list is read up to that many places behind its end.
+__device__ __forceinline__ int rank_of(const Candidate *list, Candidate c, int n) {
   int r = 0;
-  for (int j = 0; j < n; ++j) r += better(S.v[j], S.id[j], S.v[i], S.id[i]) ? 1 : 0;
+  for (int j = 0; j < n; j += RANK_STEP)
+#pragma unroll
+    for (int e = 0; e < RANK_STEP; ++e) r += list[j + e] > c ? j + e < n : 0;
   return r;
 }
 
-// The k best of columns [c0, c1): leaves at least min(k, allowed columns) of them, the best among them, in S.v / S.id and
-// returns their number.  m: this thread's maximum, LOWEST if it met none.
-//  - tau, the k-th largest of 64 maxima of disjoint sets (the quads' columns), has at least k columns at or above it, and no
-//    more than about -64 log(1 - k / 64) where the values are spread by chance: 24 of them for k = 20, 44 for k = 32.
-//  - groups whose maximum reaches tau are read again (k groups, 1 KB each, of a row of 125 or more).
-//  - where more than CAND columns pass (many equal logits: a mask of the lowest value, or an ascending row), tau is raised to the
-//    k-th largest of the CAND that were kept until the columns ABOVE it fit, and if those are fewer than k, columns equal to tau
-//    fill up from the lowest on.
+// More than CAND columns reach tau (many equal logits: a mask of the lowest value; a row in ascending order): tau is raised to the
+// k-th largest of 256 columns above it until those above it fit, and if they are fewer than k, columns equal to tau fill up,
+// from the lowest on.
 template <bool BF16>
-__device__ int best_columns(TopScratch &S, const void *row, int c0, int c1, int turns, int k, float m) {
-  using T = Turn<BF16>;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n_groups = turns * T::GROUPS;
-  m = fmaxf(m, __shfl_xor(m, 1, 64));
-  m = fmaxf(m, __shfl_xor(m, 2, 64));
-  if ((lane & 3) == 0) S.quad[threadIdx.x >> 2] = m;
-  if (threadIdx.x == 0) S.n_list = S.n_cand = 0;
-  __syncthreads();
-  if (wave == 0) {
-    const float v = S.quad[lane];
-    int r = 0;
-#pragma unroll
-    for (int j = 0; j < 64; ++j) r += better(S.quad[j], j, v, lane) ? 1 : 0;
-    if (r == k - 1) S.tau = v;
-  }
-  __syncthreads();
-  float tau = S.tau;
-  list_groups(S, n_groups, tau, false);
-  __syncthreads();
-  collect<BF16>(S, row, c0, c1, tau, false);
-  __syncthreads();
-  int n = S.n_cand;
-  if (n <= CAND) return n;
-  for (bool first = true;; first = false) {
-    if (!first) {                                // CAND columns above tau are here: their k-th best is above tau too
-      for (int i = threadIdx.x; i < CAND; i += NT)
-        if (rank_of(S, i, CAND) == k - 1) S.tau = S.v[i];
-      __syncthreads();
-      tau = S.tau;
-    }
+__device__ __noinline__ int best_columns_crowded(TopScratch &S, const void *row, int c0, int c1, int n_groups, int k, float tau) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int n;
+  for (;;) {
     __syncthreads();
     if (threadIdx.x == 0) S.n_list = S.n_cand = 0;
     __syncthreads();
-    list_groups(S, n_groups, tau, true);
-    __syncthreads();
-    collect<BF16>(S, row, c0, c1, tau, true);
-    __syncthreads();
-    n = S.n_cand;
+    n = collect<BF16>(S, row, c0, c1, n_groups, tau, true);
     if (n <= CAND) break;
+    const Candidate c = S.c[threadIdx.x];
+    if (rank_of(S.c, c, NT) == k - 1) S.tau = value_of(c);
+    __syncthreads();
+    tau = S.tau;
   }
+  const int above = n;
   for (int c = c0; c < c1 && n < k; c += NT) {
     const int col = c + threadIdx.x;
     const bool tie = col < c1 && ld_io<BF16>(row, col) == tau;
@@ -218,110 +274,170 @@ __device__ int best_columns(TopScratch &S, const void *row, int c0, int c1, int 
     if (lane == 0) S.scan[wave] = __popcll(b);
     __syncthreads();
     int at = n + __popcll(b & ((1ull << lane) - 1));
-    for (int w = 0; w < 4; ++w) {
+    for (int w = 0; w < WAVES; ++w) {
       if (w < wave) at += S.scan[w];
       n += S.scan[w];
     }
-    if (tie && at < k) { S.v[at] = tau; S.id[at] = col; }
+    if (tie && at < k) S.c[at] = candidate(tau, col);
   }
   __syncthreads();
-  return min(n, max(k, S.n_cand));
+  return min(n, max(k, above));
+}
+
+// The k best of columns [c0, c1): leaves at least min(k, allowed columns) of them, the best among them, in S.c and returns their
+// number.  m: this thread's maximum, LOWEST if it met none.
+// tau, the k-th largest of 64 maxima of disjoint sets of columns (the quads'), has at least k columns at or above it, and about
+// -64 log(1 - k / 64) where the values are spread by chance: 24 for k = 20, 44 for k = 32.  The groups whose maximum reaches tau, about as
+// many, are read again, 256 bytes each.
+// meanwhile: what the last wave does while the first looks for tau.
+template <bool BF16, typename F>
+__device__ __forceinline__ int best_columns(TopScratch &S, const void *row, int c0, int c1, int turns, int k, float m, F meanwhile) {
+  const int n_groups = turns * Turn<BF16>::GROUPS;
+  m = max_quad(m);
+  if ((threadIdx.x & 3) == 0) S.set[threadIdx.x >> 2] = m;
+  if (threadIdx.x == 0) S.n_list = S.n_cand = 0;
+  __syncthreads();
+  if (threadIdx.x < 64) {
+    const float t = kth_of_64(S.set, k);
+    if (threadIdx.x == 0) S.tau = t;
+  }
+  if (threadIdx.x >= NT - 64) meanwhile();
+  __syncthreads();
+  const float tau = S.tau;
+  const int n = collect<BF16>(S, row, c0, c1, n_groups, tau, false);
+  return n <= CAND ? n : best_columns_crowded<BF16>(S, row, c0, c1, n_groups, k, tau);
 }
 
 // Floats of the partial results of one part when a row is shared by several blocks: State, then the part's alternatives, best first.
 __host__ __device__ __forceinline__ size_t part_floats(int k) { return (size_t)(4 + 2 * k + 3) & ~(size_t)3; }
 
-// One block per row, or per part of a row where there are few rows.  One pass over the logits with the running maximum of every
-// thread: 9.5 vector instructions a logit, of which the exponential takes 4 slots.
+// A block per row, or per part of a row.  One pass over the logits with a running maximum in every thread.  The exponent of a term is one
+// fma, x log2 e - m2, with m2 the product for the maximum rounded to fp32: every term carries the factor 2^delta,
+// delta = m log2 e - m2, which is taken out at the end (it is the term of the maximum itself).
 template <bool BF16, bool TOP>
 __global__ __launch_bounds__(NT) void token_logprobs_kernel(const TokenLogprobs a, int parts, int part_turns, float *__restrict__ scratch) {
   using T = Turn<BF16>;
-  __shared__ float red[NT / 64][3];
-  __shared__ float redm[NT / 64];
+  __shared__ float red[4][WAVES];
   __shared__ typename std::conditional<TOP, TopScratch, int>::type S;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   for (long long w = blockIdx.x; w < (long long)a.n * parts; w += gridDim.x) {
     const long long r = parts == 1 ? w : w / parts;
     const int part = (int)(w - r * parts);
     const void *row = (const char *)a.logits + (size_t)r * a.ld * (BF16 ? 2 : 4);
     const int c0 = part * part_turns * T::COLS, c1 = min((long long)a.vocab, (long long)c0 + part_turns * T::COLS);
     const int turns = (c1 - c0 + T::COLS - 1) / T::COLS;
-    float x_token = 0.f;
-    if (parts == 1 && a.logp && threadIdx.x == 0) {          // asked for ahead of the row
-      const int tok = a.token_ids[r];
-      if (tok >= 0 && tok < a.vocab) x_token = ld_io<BF16>(row, tok);
-    }
-    float m = LOWEST, s = 0.f, u = 0.f;
-    for (int t = 0; t < turns; ++t) {
-      Chunk<BF16> x[U];
+    const int tok = parts == 1 && a.logp ? a.token_ids[r] : -1;          // asked for ahead of the row, used behind it
+    float m = LOWEST, m2 = -BIG * LOG2E, s = 0.f, u = 0.f;
+    Chunk<BF16> next[U];
+    const auto ask = [&](int t) {
       if (c0 + (t + 1) * T::COLS <= c1) {
 #pragma unroll
-        for (int i = 0; i < U; ++i) x[i].load(row, c0 + T::column(t, i, threadIdx.x));
+        for (int i = 0; i < U; ++i) next[i].load(row, c0 + T::column(t, i, threadIdx.x));
       } else {
 #pragma unroll
-        for (int i = 0; i < U; ++i) x[i].load_edge(row, c0 + T::column(t, i, threadIdx.x), c1);
+        for (int i = 0; i < U; ++i) next[i].load_edge(row, c0 + T::column(t, i, threadIdx.x), c1);
       }
+    };
+    ask(0);
+    for (int t = 0; t < turns; ++t) {
+      Chunk<BF16> x[U];
+#pragma unroll
+      for (int i = 0; i < U; ++i) x[i] = next[i];
+      if (t + 1 < turns) ask(t + 1);
       float g = LOWEST;
 #pragma unroll
       for (int i = 0; i < U; ++i)
 #pragma unroll
         for (int j = 0; j < T::N; ++j) g = fmaxf(g, x[i].get(j));
-      const float mn = fmaxf(m, g), d = fmaxf(m - mn, FAR), c = exp_of(d);
+      m = fmaxf(m, g);
+      const float mn = reference_of(m), d = fmaxf(m2 - mn, FAR2), c = __builtin_amdgcn_exp2f(d);
       u = c * (u + s * d);
       s *= c;
-      m = mn;
+      m2 = mn;
 #pragma unroll
       for (int i = 0; i < U; ++i)
 #pragma unroll
         for (int j = 0; j < T::N; ++j) {
-          const float y = x[i].get(j) - m, e = exp_of(y);
+          const float y = fmaf(x[i].get(j), LOG2E, -m2), e = __builtin_amdgcn_exp2f(y);
           s += e;
-          u += e * fmaxf(y, FAR);
+          u += e * fmaxf(y, FAR2);
         }
       if constexpr (TOP) {
-        g = fmaxf(g, __shfl_xor(g, 1, 64));
-        g = fmaxf(g, __shfl_xor(g, 2, 64));
+        g = max_quad(g);
         if ((threadIdx.x & 3) == 0) S.group[t * T::GROUPS + (threadIdx.x >> 2)] = g;
       }
     }
+    const bool given = tok >= 0 && tok < a.vocab;
+    const float x_token = given ? ld_io<BF16>(row, tok) : 0.f;
     State st;
-    st.m = wave_max(m);
-    if ((threadIdx.x & 63) == 0) redm[threadIdx.x >> 6] = st.m;
+    st.m = max_all(m);
+    if (lane == 0) red[3][wave] = st.m;
     __syncthreads();
+    st.m = red[3][0];
 #pragma unroll
-    for (int i = 0; i < NT / 64; ++i) st.m = fmaxf(st.m, redm[i]);
+    for (int i = 1; i < WAVES; ++i) st.m = fmaxf(st.m, red[3][i]);
+    // This thread's sums relative to its maximum, the maximum's own term (e0) left out: sum e^(x - m) = 1 + s.  A thread that met
+    // nothing near the row's maximum has none.
+    float top = m;
+    bool one;
+    if (fabsf(st.m) <= BIG) {
+      const float delta = fmaf(m, LOG2E, -m2), e0 = __builtin_amdgcn_exp2f(delta);
+      one = s > 0.f && e0 > 0.f;
+      const float inv = __builtin_amdgcn_rcpf(e0);
+      u = one ? (u - delta * s) * (LN2 * inv) : 0.f;
+      s = one ? (s - e0) * inv : s;
+    } else {                                     // again, term by term: a maximum of huge magnitude, or nothing but banned tokens
+      top = st.m;
+      s = u = 0.f;
+      for (int c = c0 + (int)threadIdx.x; c < c1; c += NT) {
+        const float y = ld_io<BF16>(row, c) - top, e = exp_of(y);
+        s += e;
+        u += e * fmaxf(y, FAR);
+      }
+      one = s >= 1.f;
+      s = one ? s - 1.f : s;
+    }
     {
-      const float d = fmaxf(m - st.m, FAR), c = exp_of(d);
-      u = c * (u + s * d);
-      s *= c;
-      const bool one = m == st.m && s >= 1.f;
-      const float3 t = block_sum3<NT>(make_float3(one ? 1.f : 0.f, one ? s - 1.f : s, u), red);
-      st.ones = t.x; st.rest = t.y; st.u = t.z;
+      const float d = fmaxf(top - st.m, FAR), c = exp_of(d), all = one ? 1.f + s : s;
+      const bool is_top = one && top == st.m;
+      st.ones = sum_all(is_top ? 1.f : 0.f);
+      st.rest = sum_all(is_top ? s : c * all);
+      st.u = sum_all(c * (u + all * d));
+      if (lane == 0) { red[0][wave] = st.ones; red[1][wave] = st.rest; red[2][wave] = st.u; }
+      __syncthreads();
+      st.ones = red[0][0]; st.rest = red[1][0]; st.u = red[2][0];
+#pragma unroll
+      for (int i = 1; i < WAVES; ++i) { st.ones += red[0][i]; st.rest += red[1][i]; st.u += red[2][i]; }
     }
     float *out = parts == 1 ? nullptr : scratch + (size_t)w * part_floats(a.top_k);
+    const bool writer = threadIdx.x == NT - 64;
     Row o = {};
-    if (parts == 1) o = finish(st, a, (size_t)r, x_token, threadIdx.x == 0);
-    else if (threadIdx.x == 0) *(float4 *)out = make_float4(st.m, st.ones, st.rest, st.u);
-    if constexpr (TOP) {
+    const auto results = [&]() {
+      if (parts == 1) o = finish(st, a, (size_t)r, given, x_token, writer);
+      else if (writer) *(float4 *)out = make_float4(st.m, st.ones, st.rest, st.u);
+    };
+    if constexpr (!TOP) {
+      if (threadIdx.x >= NT - 64) results();
+    } else {
       const int k = a.top_k;
-      const int n = best_columns<BF16>(S, row, c0, c1, turns, k, m);
-      for (int i = threadIdx.x; i < n; i += NT) {
-        const int at = rank_of(S, i, n);
+      const int n = best_columns<BF16>(S, row, c0, c1, turns, k, m, [&]() {
+        results();
+        if (writer) S.row = o;
+      });
+      o = S.row;
+      for (int i = threadIdx.x; i < max(n, k); i += NT) {
+        const bool there = i < n;                // (not: the places behind the last allowed column)
+        const Candidate c = there ? S.c[i] : 0;
+        const int at = there ? rank_of(S.c, c, n) : i;
         if (at >= k) continue;
+        const float v = there ? value_of(c) : -INFINITY;
+        const int col = there ? column_of(c) : -1;
         if (parts == 1) {
-          a.top_ids[r * k + at] = o.bad ? -1 : S.id[i];
-          if (a.top_logp) a.top_logp[r * k + at] = o.logp(S.v[i]);
+          a.top_ids[r * k + at] = o.bad ? -1 : col;
+          if (a.top_logp) a.top_logp[r * k + at] = o.bad ? NAN : there ? o.logp(v) : -INFINITY;
         } else {
-          out[4 + at] = S.v[i];
-          out[4 + k + at] = __int_as_float(S.id[i]);
-        }
-      }
-      for (int at = n + threadIdx.x; at < k; at += NT) {
-        if (parts == 1) {
-          a.top_ids[r * k + at] = -1;
-          if (a.top_logp) a.top_logp[r * k + at] = o.bad ? NAN : -INFINITY;
-        } else {
-          out[4 + at] = -INFINITY;
-          out[4 + k + at] = __int_as_float(-1);
+          out[4 + at] = v;
+          out[4 + k + at] = __int_as_float(col);
         }
       }
     }
@@ -329,46 +445,59 @@ __global__ __launch_bounds__(NT) void token_logprobs_kernel(const TokenLogprobs 
   }
 }
 
-// Joins the parts of a row: one wave per row, part p in lane p.
+// Joins the parts of a row: one block per row, part p in lane p.  Of the parts' alternatives those stay that reach the k-th best of 64
+// of them, the first few of every part.
 template <bool BF16>
-__global__ __launch_bounds__(64) void token_logprobs_join_kernel(const TokenLogprobs a, int parts, const float *__restrict__ scratch) {
-  __shared__ float lv[64 * TOP_K_MAX];
-  __shared__ int li[64 * TOP_K_MAX];
-  const int lane = threadIdx.x, k = a.top_k;
+__global__ __launch_bounds__(NT) void token_logprobs_join_kernel(const TokenLogprobs a, int parts, const float *__restrict__ scratch) {
+  constexpr int MOST = 64 * TOP_K_MAX;
+  __shared__ alignas(16) Candidate list[MOST + RANK_STEP];
+  __shared__ alignas(16) float set[64];
+  __shared__ int n_cand;
+  const int lane = threadIdx.x & 63, k = a.top_k;
+  const size_t stride = part_floats(k);
   for (long long r = blockIdx.x; r < a.n; r += gridDim.x) {
-    float x_token = 0.f;
-    if (a.logp && lane == 0) {
-      const int tok = a.token_ids[r];
-      if (tok >= 0 && tok < a.vocab) x_token = ld_io<BF16>(a.logits, (size_t)r * a.ld + tok);
-    }
-    const float *in = scratch + (size_t)r * parts * part_floats(k);
+    const int tok = a.logp ? a.token_ids[r] : -1;
+    const bool given = tok >= 0 && tok < a.vocab;
+    const float *in = scratch + (size_t)r * parts * stride;
     float4 t = make_float4(LOWEST, 0.f, 0.f, 0.f);
-    if (lane < parts) t = *(const float4 *)(in + lane * part_floats(k));
-    for (int i = lane; i < parts * k; i += 64) {
-      const int p = i / k, at = i - p * k;
-      lv[i] = in[p * part_floats(k) + 4 + at];
-      li[i] = __float_as_int(in[p * part_floats(k) + 4 + k + at]);
+    if (lane < parts) t = *(const float4 *)(in + lane * stride);
+    if (k && threadIdx.x < 64) {                 // lane p + parts * i: alternative i of part p
+      const int p = lane % parts, i = lane / parts;
+      set[lane] = i < min(k, 64 / parts) ? fmaxf(in[p * stride + 4 + i], LOWEST) : LOWEST;
+      if (lane == 0) n_cand = 0;
     }
+    const float x_token = given ? ld_io<BF16>(a.logits, (size_t)r * a.ld + tok) : 0.f;
     State st;
-    st.m = wave_max(t.x);
+    st.m = max_all(t.x);
     const float d = fmaxf(t.x - st.m, FAR), c = exp_of(d), s = t.y + t.z;
     const bool top = t.x == st.m;
-    st.u = wave_sum(c * (t.w + s * d));
-    st.ones = wave_sum(top ? t.y : 0.f);
-    st.rest = wave_sum(top ? t.z : c * s);
-    const Row o = finish(st, a, (size_t)r, x_token, lane == 0);
+    st.u = sum_all(c * (t.w + s * d));
+    st.ones = sum_all(top ? t.y : 0.f);
+    st.rest = sum_all(top ? t.z : c * s);
+    const Row o = finish(st, a, (size_t)r, given, x_token, threadIdx.x == 0);
     __syncthreads();
-    int at = 0;
-    for (int i = 0; i < k; ++i) {                // columns ascend with the part: on ties the lower lane
-      float v = lane < parts && at < k ? lv[lane * k + at] : -INFINITY;
-      const float best = wave_max(v);
-      const unsigned long long who = __ballot(v == best && best > -INFINITY);
-      const int winner = who ? __builtin_ctzll(who) : 0;
-      if (lane == winner) {
-        const bool none = !who;
-        a.top_ids[r * k + i] = none || o.bad ? -1 : li[lane * k + at];
-        if (a.top_logp) a.top_logp[r * k + i] = none && !o.bad ? -INFINITY : o.logp(v);
-        if (!none) ++at;
+    if (k) {
+      const float tau = kth_of_64(set, k);
+      for (int i0 = 0; i0 < parts * k; i0 += NT) {
+        const int i = i0 + (int)threadIdx.x, p = i / k;
+        float v = -INFINITY;
+        int col = -1;
+        if (i < parts * k) {
+          const float *y = in + p * stride + 4 + (i - p * k);
+          v = y[0];
+          col = __float_as_int(y[k]);
+        }
+        append(list, MOST, &n_cand, v >= tau, candidate(v, col));
+      }
+      __syncthreads();
+      const int n = n_cand;
+      for (int i = threadIdx.x; i < max(n, k); i += NT) {
+        const bool there = i < n;
+        const Candidate x = there ? list[i] : 0;
+        const int at = there ? rank_of(list, x, n) : i;
+        if (at >= k) continue;
+        a.top_ids[r * k + at] = there && !o.bad ? column_of(x) : -1;
+        if (a.top_logp) a.top_logp[r * k + at] = o.bad ? NAN : there ? o.logp(value_of(x)) : -INFINITY;
       }
     }
     __syncthreads();
@@ -426,13 +555,26 @@ __global__ __launch_bounds__(NT) void token_logprobs_grad_kernel(const TokenLogp
   }
 }
 
-// Parts of a row: one, unless there are too few rows to occupy the chip or a row is longer than the LDS has group maxima for.
-// Counted for fp32 whatever the type, so that the scratch does not depend on it.
+// Blocks (parts) of a row: where there are fewer than 512 rows, parts of eight turns (32768 fp32 columns), below which joining them costs more
+// than they save.  us with 20 alternatives, one part / parts of eight turns / of four: one row of 32000 fp32 logits 8.9 / 8.9 / 11.9, one
+// of 128011 20.2 / 12.8 / 11.8, 64 of 32000 9.9 / 9.9 / 13.7, 64 of 128011 28.0 / 16.5 / 18.0, 256 of 128011 41.4 / 33.9 / 37.  Counted for fp32 whatever the type, so that the scratch does not depend on it.
 int parts_of(int n, int vocab) {
-  const int turns = (vocab + Turn<false>::COLS - 1) / Turn<false>::COLS;
-  int parts = (turns + MAX_TURNS - 1) / MAX_TURNS;
-  if (n < 512) parts = std::max(parts, std::min({1024 / n, turns, 64}));
-  return parts;
+  using T = Turn<false>;
+  const int turns = (vocab + T::COLS - 1) / T::COLS, least = (turns + T::MAX_TURNS - 1) / T::MAX_TURNS;
+  return std::max(least, std::min({512 / n, turns / 8, 64}));
+}
+
+template <bool BF16>
+hipError_t launch_rows(const TokenLogprobs &a, float *scratch, hipStream_t st) {
+  using T = Turn<BF16>;
+  int parts = parts_of(a.n, a.vocab);
+  const int turns = (a.vocab + T::COLS - 1) / T::COLS, part_turns = (turns + parts - 1) / parts;
+  parts = (turns + part_turns - 1) / part_turns;
+  const dim3 grid((unsigned)std::min<long long>((long long)a.n * parts, 1 << 22));
+  auto *k = a.top_k ? token_logprobs_kernel<BF16, true> : token_logprobs_kernel<BF16, false>;
+  hipLaunchKernelGGL(k, grid, dim3(NT), 0, st, a, parts, part_turns, scratch);
+  if (parts > 1) hipLaunchKernelGGL(token_logprobs_join_kernel<BF16>, dim3((unsigned)std::min(a.n, 1 << 22)), dim3(NT), 0, st, a, parts, (const float *)scratch);
+  return hipGetLastError();
 }
 
 }  // namespace
@@ -445,19 +587,7 @@ size_t token_logprobs_scratch_bytes(int n, int vocab, int top_k) {
 
 hipError_t launch_token_logprobs(const TokenLogprobs &a, bool bf16, void *scratch, hipStream_t st) {
   if (a.n <= 0) return hipSuccess;
-  int parts = parts_of(a.n, a.vocab);
-  const int cols = bf16 ? Turn<true>::COLS : Turn<false>::COLS, turns = (a.vocab + cols - 1) / cols, part_turns = (turns + parts - 1) / parts;
-  parts = (turns + part_turns - 1) / part_turns;
-  const dim3 grid((unsigned)std::min<long long>((long long)a.n * parts, 1 << 22));
-  auto *k = bf16 ? (a.top_k ? token_logprobs_kernel<true, true> : token_logprobs_kernel<true, false>)
-                 : (a.top_k ? token_logprobs_kernel<false, true> : token_logprobs_kernel<false, false>);
-  hipLaunchKernelGGL(k, grid, dim3(NT), 0, st, a, parts, part_turns, (float *)scratch);
-  if (parts > 1) {
-    const dim3 rows((unsigned)std::min(a.n, 1 << 22));
-    if (bf16) hipLaunchKernelGGL(token_logprobs_join_kernel<true>, rows, dim3(64), 0, st, a, parts, (const float *)scratch);
-    else hipLaunchKernelGGL(token_logprobs_join_kernel<false>, rows, dim3(64), 0, st, a, parts, (const float *)scratch);
-  }
-  return hipGetLastError();
+  return bf16 ? launch_rows<true>(a, (float *)scratch, st) : launch_rows<false>(a, (float *)scratch, st);
 }
 
 hipError_t launch_token_logprobs_grad(const TokenLogprobsGrad &a, bool bf16, bool out_bf16, hipStream_t st) {
