@@ -29,14 +29,19 @@ struct Chunk {
   static constexpr int N = BF16 ? 8 : 4;
   typedef typename std::conditional<BF16, u32x4_a2, u32x4_a4>::type raw_t;
   raw_t raw;
-  __device__ __forceinline__ void load(const void *row, int col) { raw = *(const raw_t *)((const char *)row + (size_t)col * (BF16 ? 2 : 4)); }
+  template <bool STREAM>
+  __device__ __forceinline__ void load(const void *row, int col) {
+    const raw_t *p = (const raw_t *)((const char *)row + (size_t)col * (BF16 ? 2 : 4));
+    if constexpr (STREAM) raw = __builtin_nontemporal_load(p);
+    else raw = *p;
+  }
   __device__ __forceinline__ float get(int i) const {
     if constexpr (BF16) return __uint_as_float(i & 1 ? raw[i >> 1] & 0xffff0000u : raw[i >> 1] << 16);
     else return __uint_as_float(raw[i]);
   }
   // columns col .. col + N - 1, -inf from `end` on
   __device__ __forceinline__ void load_edge(const void *row, int col, int end) {
-    if (col + N <= end) return load(row, col);
+    if (col + N <= end) return load<false>(row, col);
     uint32_t w[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -122,17 +127,16 @@ __device__ __forceinline__ Row finish(const State &t, const TokenLogprobs &a, si
   return o;
 }
 
-constexpr int NT = 256, WAVES = NT / 64;         // threads and waves of a block
 constexpr int U = 4;                             // 16-byte accesses of a thread in a turn
-constexpr int MAX_GROUPS = 2048;                 // group maxima that LDS holds: 131072 fp32 columns of a part
-constexpr int CAND = 1024;                       // candidates for the alternatives that LDS holds
 constexpr int RANK_STEP = 8;
 
-// A turn is NT * U consecutive 16-byte accesses; the four lanes of a quad hold U x 64 bytes of it, a group, whose maximum is
-// kept: the alternatives are then found without a second pass over the row.
-template <bool BF16>
+// A turn of a block of NT threads is NT * U consecutive 16-byte accesses; the four lanes of a quad hold U x 64 bytes of it, a group,
+// whose maximum is kept: the alternatives are then found without a second pass over the row.  MAX_GROUPS maxima fit the LDS (131072
+// fp32 columns of a part with 256 threads, 8192 with 64), and CAND candidates.
+template <bool BF16, int NT>
 struct Turn {
-  static constexpr int N = Chunk<BF16>::N, COLS = NT * U * N, GROUPS = NT / 4, GROUP_COLS = 4 * U * N, MAX_TURNS = MAX_GROUPS / GROUPS;
+  static constexpr int N = Chunk<BF16>::N, COLS = NT * U * N, GROUPS = NT / 4, GROUP_COLS = 4 * U * N;
+  static constexpr int WAVES = NT / 64, MAX_GROUPS = NT == 64 ? 128 : 2048, MAX_TURNS = MAX_GROUPS / GROUPS, CAND = NT == 64 ? 512 : 1024;
   static __device__ __forceinline__ int column(int turn, int u, int thread) { return turn * COLS + (u * NT + thread) * N; }
 };
 
@@ -148,12 +152,14 @@ __device__ __forceinline__ float value_of(Candidate c) {
   return __uint_as_float(b & 0x80000000u ? b ^ 0x80000000u : ~b);
 }
 __device__ __forceinline__ int column_of(Candidate c) { return (int)~(uint32_t)c; }
+template <int NT>
 struct TopScratch {
-  alignas(16) Candidate c[CAND + RANK_STEP];
-  float group[MAX_GROUPS];
-  uint16_t list[MAX_GROUPS];
+  using T = Turn<false, NT>;
+  alignas(16) Candidate c[T::CAND + RANK_STEP];
+  float group[T::MAX_GROUPS];
+  uint16_t list[T::MAX_GROUPS];
   alignas(16) float set[64];
-  int n_list, n_cand, scan[WAVES];
+  int n_list, n_cand, scan[T::WAVES];
   float tau;
   Row row;
 };
@@ -169,7 +175,7 @@ __device__ __forceinline__ void append(T *list, int most, int *n, bool pass, T i
   if (pass && at < most) list[at] = item;
 }
 
-// The k-th largest of 64 values (LOWEST where there is none), one in every lane; k <= 64.
+// The k-th largest of 64 values, at least the lowest finite one; k <= 64.
 __device__ __forceinline__ float kth_of_64(const float *set, int k) {
   const float v = set[threadIdx.x & 63];
   int above = 0;
@@ -181,19 +187,21 @@ __device__ __forceinline__ float kth_of_64(const float *set, int k) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) above += (w[i].x > v) + (w[i].y > v) + (w[i].z > v) + (w[i].w > v);
   }
-  return -max_all(above < k ? -v : -INFINITY);   // the least of those with fewer than k above them
+  return fmaxf(-max_all(above < k ? -v : -INFINITY), LOWEST);      // the least of those with fewer than k above them
 }
 
 // Leaves the columns whose value passes (strict ? > : >=) tau in S.c and returns their number, of which S.c holds CAND: lists the
 // groups whose maximum passes, and reads those again, eight loads of a wave at a time.
-template <bool BF16>
-__device__ __forceinline__ int collect(TopScratch &S, const void *row, int c0, int c1, int n_groups, float tau, bool strict) {
-  using T = Turn<BF16>;
+template <bool BF16, int NT>
+__device__ __forceinline__ int collect(TopScratch<NT> &S, const void *row, int c0, int c1, int n_groups, float tau, bool strict) {
+  using T = Turn<BF16, NT>;
+  constexpr int WAVES = T::WAVES, CAND = T::CAND;
   constexpr int PER = T::GROUP_COLS / 64, AT_ONCE = 8 / PER;    // adjacent columns of a lane and group; groups
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  for (int g = threadIdx.x; g < n_groups; g += NT) {            // n_groups is a multiple of 64
-    const float v = S.group[g];
-    append(S.list, MAX_GROUPS, &S.n_list, strict ? v > tau : v >= tau, (uint16_t)g);
+  for (int g0 = 0; g0 < n_groups; g0 += NT) {
+    const int g = g0 + (int)threadIdx.x;
+    const float v = g < n_groups ? S.group[g] : NAN;
+    append(S.list, T::MAX_GROUPS, &S.n_list, strict ? v > tau : v >= tau, (uint16_t)g);
   }
   __syncthreads();
   const int n = S.n_list;
@@ -248,17 +256,18 @@ __device__ __forceinline__ int rank_of(const Candidate *list, Candidate c, int n
 }
 
 // More than CAND columns reach tau (many equal logits: a mask of the lowest value; a row in ascending order): tau is raised to the
-// k-th largest of 256 columns above it until those above it fit, and if they are fewer than k, columns equal to tau fill up,
+// k-th largest of NT columns above it until those above it fit, and if they are fewer than k, columns equal to tau fill up,
 // from the lowest on.
-template <bool BF16>
-__device__ __noinline__ int best_columns_crowded(TopScratch &S, const void *row, int c0, int c1, int n_groups, int k, float tau) {
+template <bool BF16, int NT>
+__device__ __noinline__ int best_columns_crowded(TopScratch<NT> &S, const void *row, int c0, int c1, int n_groups, int k, float tau) {
+  constexpr int WAVES = NT / 64, CAND = Turn<BF16, NT>::CAND;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   int n;
   for (;;) {
     __syncthreads();
     if (threadIdx.x == 0) S.n_list = S.n_cand = 0;
     __syncthreads();
-    n = collect<BF16>(S, row, c0, c1, n_groups, tau, true);
+    n = collect<BF16, NT>(S, row, c0, c1, n_groups, tau, true);
     if (n <= CAND) break;
     const Candidate c = S.c[threadIdx.x];
     if (rank_of(S.c, c, NT) == k - 1) S.tau = value_of(c);
@@ -285,16 +294,18 @@ __device__ __noinline__ int best_columns_crowded(TopScratch &S, const void *row,
 }
 
 // The k best of columns [c0, c1): leaves at least min(k, allowed columns) of them, the best among them, in S.c and returns their
-// number.  m: this thread's maximum, LOWEST if it met none.
-// tau, the k-th largest of 64 maxima of disjoint sets of columns (the quads'), has at least k columns at or above it, and about
+// number.  m: this thread's maximum, -inf if it met none.
+// tau, the k-th largest of 64 maxima of disjoint sets of columns (a quad's, or a lane's), has at least k columns at or above it, and about
 // -64 log(1 - k / 64) where the values are spread by chance: 24 for k = 20, 44 for k = 32.  The groups whose maximum reaches tau, about as
 // many, are read again, 256 bytes each.
 // meanwhile: what the last wave does while the first looks for tau.
-template <bool BF16, typename F>
-__device__ __forceinline__ int best_columns(TopScratch &S, const void *row, int c0, int c1, int turns, int k, float m, F meanwhile) {
-  const int n_groups = turns * Turn<BF16>::GROUPS;
-  m = max_quad(m);
-  if ((threadIdx.x & 3) == 0) S.set[threadIdx.x >> 2] = m;
+template <bool BF16, int NT, typename F>
+__device__ __forceinline__ int best_columns(TopScratch<NT> &S, const void *row, int c0, int c1, int turns, int k, float m, F meanwhile) {
+  using T = Turn<BF16, NT>;
+  constexpr int SET = NT / 64;                   // threads of a set
+  const int n_groups = turns * T::GROUPS;
+  if (SET > 1) m = max_quad(m);
+  if (threadIdx.x % SET == 0) S.set[threadIdx.x / SET] = m;
   if (threadIdx.x == 0) S.n_list = S.n_cand = 0;
   __syncthreads();
   if (threadIdx.x < 64) {
@@ -304,8 +315,8 @@ __device__ __forceinline__ int best_columns(TopScratch &S, const void *row, int 
   if (threadIdx.x >= NT - 64) meanwhile();
   __syncthreads();
   const float tau = S.tau;
-  const int n = collect<BF16>(S, row, c0, c1, n_groups, tau, false);
-  return n <= CAND ? n : best_columns_crowded<BF16>(S, row, c0, c1, n_groups, k, tau);
+  const int n = collect<BF16, NT>(S, row, c0, c1, n_groups, tau, false);
+  return n <= T::CAND ? n : best_columns_crowded<BF16, NT>(S, row, c0, c1, n_groups, k, tau);
 }
 
 // Floats of the partial results of one part when a row is shared by several blocks: State, then the part's alternatives, best first.
@@ -314,11 +325,12 @@ __host__ __device__ __forceinline__ size_t part_floats(int k) { return (size_t)(
 // A block per row, or per part of a row.  One pass over the logits with a running maximum in every thread.  The exponent of a term is one
 // fma, x log2 e - m2, with m2 the product for the maximum rounded to fp32: every term carries the factor 2^delta,
 // delta = m log2 e - m2, which is taken out at the end (it is the term of the maximum itself).
-template <bool BF16, bool TOP>
-__global__ __launch_bounds__(NT) void token_logprobs_kernel(const TokenLogprobs a, int parts, int part_turns, float *__restrict__ scratch) {
-  using T = Turn<BF16>;
+template <bool BF16, bool TOP, int NT, bool STREAM>
+__global__ __launch_bounds__(NT, NT == 64 ? 5 : 1) void token_logprobs_kernel(const TokenLogprobs a, int parts, int part_turns, float *__restrict__ scratch) {
+  using T = Turn<BF16, NT>;
+  constexpr int WAVES = T::WAVES;
   __shared__ float red[4][WAVES];
-  __shared__ typename std::conditional<TOP, TopScratch, int>::type S;
+  __shared__ typename std::conditional<TOP, TopScratch<NT>, int>::type S;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   for (long long w = blockIdx.x; w < (long long)a.n * parts; w += gridDim.x) {
     const long long r = parts == 1 ? w : w / parts;
@@ -327,12 +339,12 @@ __global__ __launch_bounds__(NT) void token_logprobs_kernel(const TokenLogprobs 
     const int c0 = part * part_turns * T::COLS, c1 = min((long long)a.vocab, (long long)c0 + part_turns * T::COLS);
     const int turns = (c1 - c0 + T::COLS - 1) / T::COLS;
     const int tok = parts == 1 && a.logp ? a.token_ids[r] : -1;          // asked for ahead of the row, used behind it
-    float m = LOWEST, m2 = -BIG * LOG2E, s = 0.f, u = 0.f;
+    float m = -INFINITY, m2 = -BIG * LOG2E, s = 0.f, u = 0.f;
     Chunk<BF16> next[U];
     const auto ask = [&](int t) {
       if (c0 + (t + 1) * T::COLS <= c1) {
 #pragma unroll
-        for (int i = 0; i < U; ++i) next[i].load(row, c0 + T::column(t, i, threadIdx.x));
+        for (int i = 0; i < U; ++i) next[i].template load<STREAM>(row, c0 + T::column(t, i, threadIdx.x));
       } else {
 #pragma unroll
         for (int i = 0; i < U; ++i) next[i].load_edge(row, c0 + T::column(t, i, threadIdx.x), c1);
@@ -344,7 +356,7 @@ __global__ __launch_bounds__(NT) void token_logprobs_kernel(const TokenLogprobs 
 #pragma unroll
       for (int i = 0; i < U; ++i) x[i] = next[i];
       if (t + 1 < turns) ask(t + 1);
-      float g = LOWEST;
+      float g = -INFINITY;
 #pragma unroll
       for (int i = 0; i < U; ++i)
 #pragma unroll
@@ -380,19 +392,25 @@ __global__ __launch_bounds__(NT) void token_logprobs_kernel(const TokenLogprobs 
     // nothing near the row's maximum has none.
     float top = m;
     bool one;
-    if (fabsf(st.m) <= BIG) {
+    if (fabsf(st.m) <= BIG || st.m == -INFINITY) {          // (-inf: nothing but banned tokens, no term is there)
       const float delta = fmaf(m, LOG2E, -m2), e0 = __builtin_amdgcn_exp2f(delta);
       one = s > 0.f && e0 > 0.f;
       const float inv = __builtin_amdgcn_rcpf(e0);
       u = one ? (u - delta * s) * (LN2 * inv) : 0.f;
       s = one ? (s - e0) * inv : s;
-    } else {                                     // again, term by term: a maximum of huge magnitude, or nothing but banned tokens
+    } else {                                     // a maximum of huge magnitude: again, with differences of the logits themselves
       top = st.m;
       s = u = 0.f;
-      for (int c = c0 + (int)threadIdx.x; c < c1; c += NT) {
-        const float y = ld_io<BF16>(row, c) - top, e = exp_of(y);
-        s += e;
-        u += e * fmaxf(y, FAR);
+      for (int t = 0; t < turns; ++t) {
+        ask(t);
+#pragma unroll
+        for (int i = 0; i < U; ++i)
+#pragma unroll
+          for (int j = 0; j < T::N; ++j) {
+            const float y = next[i].get(j) - top, e = exp_of(y);
+            s += e;
+            u += e * fmaxf(y, FAR);
+          }
       }
       one = s >= 1.f;
       s = one ? s - 1.f : s;
@@ -420,7 +438,7 @@ __global__ __launch_bounds__(NT) void token_logprobs_kernel(const TokenLogprobs 
       if (threadIdx.x >= NT - 64) results();
     } else {
       const int k = a.top_k;
-      const int n = best_columns<BF16>(S, row, c0, c1, turns, k, m, [&]() {
+      const int n = best_columns<BF16, NT>(S, row, c0, c1, turns, k, m, [&]() {
         results();
         if (writer) S.row = o;
       });
@@ -447,8 +465,10 @@ __global__ __launch_bounds__(NT) void token_logprobs_kernel(const TokenLogprobs 
 
 // Joins the parts of a row: one block per row, part p in lane p.  Of the parts' alternatives those stay that reach the k-th best of 64
 // of them, the first few of every part.
+constexpr size_t LLC_BYTES = (size_t)256 << 20;
+constexpr int JOIN_NT = 256;
 template <bool BF16>
-__global__ __launch_bounds__(NT) void token_logprobs_join_kernel(const TokenLogprobs a, int parts, const float *__restrict__ scratch) {
+__global__ __launch_bounds__(JOIN_NT) void token_logprobs_join_kernel(const TokenLogprobs a, int parts, const float *__restrict__ scratch) {
   constexpr int MOST = 64 * TOP_K_MAX;
   __shared__ alignas(16) Candidate list[MOST + RANK_STEP];
   __shared__ alignas(16) float set[64];
@@ -459,11 +479,11 @@ __global__ __launch_bounds__(NT) void token_logprobs_join_kernel(const TokenLogp
     const int tok = a.logp ? a.token_ids[r] : -1;
     const bool given = tok >= 0 && tok < a.vocab;
     const float *in = scratch + (size_t)r * parts * stride;
-    float4 t = make_float4(LOWEST, 0.f, 0.f, 0.f);
+    float4 t = make_float4(-INFINITY, 0.f, 0.f, 0.f);
     if (lane < parts) t = *(const float4 *)(in + lane * stride);
     if (k && threadIdx.x < 64) {                 // lane p + parts * i: alternative i of part p
       const int p = lane % parts, i = lane / parts;
-      set[lane] = i < min(k, 64 / parts) ? fmaxf(in[p * stride + 4 + i], LOWEST) : LOWEST;
+      set[lane] = i < min(k, 64 / parts) ? in[p * stride + 4 + i] : -INFINITY;
       if (lane == 0) n_cand = 0;
     }
     const float x_token = given ? ld_io<BF16>(a.logits, (size_t)r * a.ld + tok) : 0.f;
@@ -478,7 +498,7 @@ __global__ __launch_bounds__(NT) void token_logprobs_join_kernel(const TokenLogp
     __syncthreads();
     if (k) {
       const float tau = kth_of_64(set, k);
-      for (int i0 = 0; i0 < parts * k; i0 += NT) {
+      for (int i0 = 0; i0 < parts * k; i0 += JOIN_NT) {
         const int i = i0 + (int)threadIdx.x, p = i / k;
         float v = -INFINITY;
         int col = -1;
@@ -491,7 +511,7 @@ __global__ __launch_bounds__(NT) void token_logprobs_join_kernel(const TokenLogp
       }
       __syncthreads();
       const int n = n_cand;
-      for (int i = threadIdx.x; i < max(n, k); i += NT) {
+      for (int i = threadIdx.x; i < max(n, k); i += JOIN_NT) {
         const bool there = i < n;
         const Candidate x = there ? list[i] : 0;
         const int at = there ? rank_of(list, x, n) : i;
@@ -504,52 +524,52 @@ __global__ __launch_bounds__(NT) void token_logprobs_join_kernel(const TokenLogp
   }
 }
 
-// Blocks share the rows' columns, GRAD_U 16-byte accesses of a thread each; HBM-bound, one read and one write a logit.
-constexpr int GRAD_U = 8;
-template <bool BF16, bool OUT_BF16>
-__global__ __launch_bounds__(NT) void token_logprobs_grad_kernel(const TokenLogprobsGrad a, int parts) {
+template <typename V, bool STREAM>
+__device__ __forceinline__ void put(char *out, size_t at, V v) {
+  if constexpr (STREAM) __builtin_nontemporal_store(v, (V *)(out + at));
+  else *(V *)(out + at) = v;
+}
+// A wave takes 64 x U 16-byte accesses of a row; HBM-bound, one read and one write a logit.
+template <bool BF16, bool OUT_BF16, bool STREAM>
+__global__ __launch_bounds__(256) void token_logprobs_grad_kernel(const TokenLogprobsGrad a, int parts) {
   constexpr int N = Chunk<BF16>::N;
-  for (long long w = blockIdx.x; w < (long long)a.n * parts; w += gridDim.x) {
+  const int lane = threadIdx.x & 63;
+  for (long long w = (long long)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); w < (long long)a.n * parts; w += (long long)gridDim.x * 4) {
     const long long r = parts == 1 ? w : w / parts;
-    const int part = (int)(w - r * parts);
+    const int c0 = (int)(w - r * parts) * 64 * U * N;
     const int tok = a.d_logp ? a.token_ids[r] : -1;
     const float g = tok >= 0 && tok < a.vocab ? a.d_logp[r] : 0.f, h = a.d_entropy ? a.d_entropy[r] : 0.f;
     const float m = a.row_stats[2 * r], L = a.row_stats[2 * r + 1], H = a.d_entropy ? a.entropy[r] : 0.f;
     const bool zero = m == -INFINITY || (g == 0.f && h == 0.f);
     const void *row = (const char *)a.logits + (size_t)r * a.ld * (BF16 ? 2 : 4);
     char *out = (char *)a.d_logits + (size_t)r * a.ld_d * (OUT_BF16 ? 2 : 4);
+    Chunk<BF16> x[U];
+    if (!zero) {
 #pragma unroll
-    for (int half = 0; half < GRAD_U / 4; ++half) {
-      Chunk<BF16> x[4];
-      const int base = (part * GRAD_U + half * 4) * NT * N;
-      if (base >= a.vocab) break;
-      if (!zero) {
+      for (int i = 0; i < U; ++i) x[i].load_edge(row, c0 + (i * 64 + lane) * N, a.vocab);
+    }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) x[i].load_edge(row, base + (i * NT + (int)threadIdx.x) * N, a.vocab);
+    for (int i = 0; i < U; ++i) {
+      const int col = c0 + (i * 64 + lane) * N;
+      float o[N];
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        if (zero) { o[j] = 0.f; continue; }
+        const float lp = x[i].get(j) - m - L, p = exp_of(lp);
+        o[j] = (col + j == tok ? g : 0.f) - g * p - h * p * (fmaxf(lp, FAR) + H);
       }
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int col = base + (i * NT + (int)threadIdx.x) * N;
-        float o[N];
-#pragma unroll
-        for (int j = 0; j < N; ++j) {
-          if (zero) { o[j] = 0.f; continue; }
-          const float lp = x[i].get(j) - m - L, p = exp_of(lp);
-          o[j] = (col + j == tok ? g : 0.f) - g * p - h * p * (fmaxf(lp, FAR) + H);
-        }
-        if (col + N <= a.vocab) {
-          if constexpr (OUT_BF16) {
-            if constexpr (BF16) *(u32x4_a2 *)(out + (size_t)col * 2) = u32x4_a2{cvt_pk_bf16(o[0], o[1]), cvt_pk_bf16(o[2], o[3]), cvt_pk_bf16(o[4], o[5]), cvt_pk_bf16(o[6], o[7])};
-            else *(u32x2_a2 *)(out + (size_t)col * 2) = u32x2_a2{cvt_pk_bf16(o[0], o[1]), cvt_pk_bf16(o[2], o[3])};
-          } else {
-#pragma unroll
-            for (int j = 0; j < N; j += 4) *(f32x4_a4 *)(out + (size_t)(col + j) * 4) = f32x4_a4{o[j], o[j + 1], o[j + 2], o[j + 3]};
-          }
+      if (col + N <= a.vocab) {
+        if constexpr (OUT_BF16) {
+          if constexpr (BF16) put<u32x4_a2, STREAM>(out, (size_t)col * 2, u32x4_a2{cvt_pk_bf16(o[0], o[1]), cvt_pk_bf16(o[2], o[3]), cvt_pk_bf16(o[4], o[5]), cvt_pk_bf16(o[6], o[7])});
+          else put<u32x2_a2, STREAM>(out, (size_t)col * 2, u32x2_a2{cvt_pk_bf16(o[0], o[1]), cvt_pk_bf16(o[2], o[3])});
         } else {
 #pragma unroll
-          for (int j = 0; j < N; ++j)
-            if (col + j < a.vocab) st_io<OUT_BF16>(out, col + j, o[j]);
+          for (int j = 0; j < N; j += 4) put<f32x4_a4, STREAM>(out, (size_t)(col + j) * 4, f32x4_a4{o[j], o[j + 1], o[j + 2], o[j + 3]});
         }
+      } else {
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+          if (col + j < a.vocab) st_io<OUT_BF16>(out, col + j, o[j]);
       }
     }
   }
@@ -559,22 +579,35 @@ __global__ __launch_bounds__(NT) void token_logprobs_grad_kernel(const TokenLogp
 // than they save.  us with 20 alternatives, one part / parts of eight turns / of four: one row of 32000 fp32 logits 8.9 / 8.9 / 11.9, one
 // of 128011 20.2 / 12.8 / 11.8, 64 of 32000 9.9 / 9.9 / 13.7, 64 of 128011 28.0 / 16.5 / 18.0, 256 of 128011 41.4 / 33.9 / 37.  Counted for fp32 whatever the type, so that the scratch does not depend on it.
 int parts_of(int n, int vocab) {
-  using T = Turn<false>;
+  using T = Turn<false, 256>;
   const int turns = (vocab + T::COLS - 1) / T::COLS, least = (turns + T::MAX_TURNS - 1) / T::MAX_TURNS;
   return std::max(least, std::min({512 / n, turns / 8, 64}));
 }
 
-template <bool BF16>
-hipError_t launch_rows(const TokenLogprobs &a, float *scratch, hipStream_t st) {
-  using T = Turn<BF16>;
-  int parts = parts_of(a.n, a.vocab);
+template <bool BF16, int NT>
+hipError_t launch_rows(const TokenLogprobs &a, int parts, float *scratch, hipStream_t st) {
+  using T = Turn<BF16, NT>;
   const int turns = (a.vocab + T::COLS - 1) / T::COLS, part_turns = (turns + parts - 1) / parts;
   parts = (turns + part_turns - 1) / part_turns;
+  // Logits that the last-level cache (256 MB) cannot hold are read past it: 16384 x 32000 fp32 354 -> 317 us, 2048 x 32000 49.0 -> 42.5; of
+  // fewer the cache may hold what their producer left (512 x 32000, resident: 12.6 -> 13.3).
+  const bool stream = (size_t)a.n * a.vocab * (BF16 ? 2 : 4) > LLC_BYTES;
   const dim3 grid((unsigned)std::min<long long>((long long)a.n * parts, 1 << 22));
-  auto *k = a.top_k ? token_logprobs_kernel<BF16, true> : token_logprobs_kernel<BF16, false>;
+  auto *k = a.top_k ? (stream ? token_logprobs_kernel<BF16, true, NT, true> : token_logprobs_kernel<BF16, true, NT, false>)
+                    : (stream ? token_logprobs_kernel<BF16, false, NT, true> : token_logprobs_kernel<BF16, false, NT, false>);
   hipLaunchKernelGGL(k, grid, dim3(NT), 0, st, a, parts, part_turns, scratch);
-  if (parts > 1) hipLaunchKernelGGL(token_logprobs_join_kernel<BF16>, dim3((unsigned)std::min(a.n, 1 << 22)), dim3(NT), 0, st, a, parts, (const float *)scratch);
+  if (parts > 1) hipLaunchKernelGGL(token_logprobs_join_kernel<BF16>, dim3((unsigned)std::min(a.n, 1 << 22)), dim3(JOIN_NT), 0, st, a, parts, (const float *)scratch);
   return hipGetLastError();
+}
+template <bool BF16>
+hipError_t launch_rows(const TokenLogprobs &a, float *scratch, hipStream_t st) {
+  const int parts = parts_of(a.n, a.vocab);
+  // A wave per row for many short rows, and for rows so short that the quads of 256 threads hold fewer sets than there are alternatives.
+  // us with 256 threads / one wave, without and with 20 alternatives: 2048 x 2048 fp32 6.9 / 5.8, 16.2 / 13.4; 8192 x 4000 26.3 / 26.4, 63.2 / 49.6;
+  // 30000 x 7000 146 / 152, 235 / 204; but 512 x 2048 3.9 / 4.3, 7.4 / 10.3.  64 x 500 bf16 with 20 alternatives 30.8 / 10.7.
+  const int few = 128 * Turn<BF16, 256>::N;      // 32 quads with a column
+  const bool wave = parts == 1 && (a.vocab <= few || (a.n >= 2048 && a.vocab <= 8192));
+  return wave ? launch_rows<BF16, 64>(a, 1, scratch, st) : launch_rows<BF16, 256>(a, parts, scratch, st);
 }
 
 }  // namespace
@@ -592,9 +625,13 @@ hipError_t launch_token_logprobs(const TokenLogprobs &a, bool bf16, void *scratc
 
 hipError_t launch_token_logprobs_grad(const TokenLogprobsGrad &a, bool bf16, bool out_bf16, hipStream_t st) {
   if (a.n <= 0) return hipSuccess;
-  const int cols = GRAD_U * NT * (bf16 ? 8 : 4), parts = (a.vocab + cols - 1) / cols;
-  auto *k = bf16 ? (out_bf16 ? token_logprobs_grad_kernel<true, true> : token_logprobs_grad_kernel<true, false>)
-                 : (out_bf16 ? token_logprobs_grad_kernel<false, true> : token_logprobs_grad_kernel<false, false>);
-  hipLaunchKernelGGL(k, dim3((unsigned)std::min<long long>((long long)a.n * parts, 1 << 22)), dim3(NT), 0, st, a, parts);
+  const int cols = 64 * U * (bf16 ? 8 : 4), parts = (a.vocab + cols - 1) / cols;
+  // Gradients that the last-level cache cannot hold are written past it: 16384 x 32000 bf16 555 -> 536 us.
+  const bool stream = (size_t)a.n * a.vocab * (out_bf16 ? 2 : 4) > LLC_BYTES;
+  auto *k = bf16 ? (out_bf16 ? (stream ? token_logprobs_grad_kernel<true, true, true> : token_logprobs_grad_kernel<true, true, false>)
+                             : (stream ? token_logprobs_grad_kernel<true, false, true> : token_logprobs_grad_kernel<true, false, false>))
+                 : (out_bf16 ? (stream ? token_logprobs_grad_kernel<false, true, true> : token_logprobs_grad_kernel<false, true, false>)
+                             : (stream ? token_logprobs_grad_kernel<false, false, true> : token_logprobs_grad_kernel<false, false, false>));
+  hipLaunchKernelGGL(k, dim3((unsigned)std::min<long long>(((long long)a.n * parts + 3) / 4, 1 << 22)), dim3(256), 0, st, a, parts);
   return hipGetLastError();
 }
