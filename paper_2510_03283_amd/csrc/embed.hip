@@ -12,7 +12,8 @@ constexpr size_t LLC_BYTES = (size_t)256 << 20;      // last-level cache
 
 // ------------------------------------------------------------------ rows
 typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
-// 2^lg threads per row, 16-byte accesses, up to four of them in flight a thread.
+// 2^lg threads per row, 16-byte accesses, four of them in flight a thread.  No branch around a load (a place behind the row reads its last one
+// again, padding reads row 0): 66576 x 4096 bf16 145 -> 131 us, 5.05 TB/s.  Fewer blocks that go on to further rows were slower (2048: 147).
 template <bool BF16, bool STREAM>
 __global__ __launch_bounds__(256) void embed_rows_kernel(const void *__restrict__ table, const int32_t *__restrict__ ids, int n, int vocab, int d,
                                                          float scale, void *__restrict__ out, int lg) {
@@ -26,7 +27,7 @@ __global__ __launch_bounds__(256) void embed_rows_kernel(const void *__restrict_
       u32x4_t x[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i)
-        if (there && k0 + i * per < vecs) x[i] = src[k0 + i * per];
+        x[i] = src[min(k0 + i * per, vecs - 1)];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         if (k0 + i * per >= vecs) break;
@@ -240,6 +241,78 @@ __global__ __launch_bounds__(64 * WAVES) void embed_place_kernel(const int32_t *
 
 constexpr int STRIP = 256, R = 8;     // columns of a wave, rows that it asks for together
 constexpr int ZERO_ROWS = 8;          // rows of the table that a wave looks at for zeros
+template <bool PAST>
+__device__ __forceinline__ void put_zero(float *to) {
+  const f32x4_t z = {0.f, 0.f, 0.f, 0.f};
+  if constexpr (PAST) __builtin_nontemporal_store(z, (f32x4_t *)to);
+  else *(f32x4_t *)to = z;
+}
+
+// The whole gradient of at most FEW_ROWS rows in one launch instead of three (us, 32 rows of 4096 9.8 -> 3.5, 256 rows 11.7 -> 4.7; 256 rows of one
+// token, the longest sum, 16.9 -> 29.7).  A unit is (row, strip of 256 columns): the first row of a token sums all of them, by looking
+// through the ids; or (ZERO_ROWS tokens, strip) behind the rows' units.
+constexpr int FEW_ROWS = 256;
+template <bool ACC, bool PAST>
+__global__ __launch_bounds__(256) void embed_few_kernel(const int32_t *__restrict__ ids, int n, const float *__restrict__ dx, int vocab, int d, float scale,
+                                                        float *__restrict__ d_table, int strips) {
+  constexpr int TURNS = FEW_ROWS / 64;
+  const int lane = threadIdx.x & 63;
+  const long long units = (n + (ACC ? 0 : ((long long)vocab + ZERO_ROWS - 1) / ZERO_ROWS)) * strips;
+  int id[TURNS];
+#pragma unroll
+  for (int t = 0; t < TURNS; ++t) id[t] = 64 * t + lane < n ? ids[64 * t + lane] : -1;
+  for (long long unit = (long long)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); unit < units; unit += (long long)gridDim.x * 4) {
+    const long long row = unit / strips;
+    const int col = (int)(unit - row * strips) * STRIP + 4 * lane;
+    const bool live = col < d;                   // other lanes of the last strip read its last column again and write nothing
+    const int at_col = live ? col : d - 4;
+    if (!ACC && row >= n) {
+      const int v0 = (int)(row - n) * ZERO_ROWS;
+      for (int i = 0; i < ZERO_ROWS && v0 + i < vocab; ++i) {
+        bool has = false;
+#pragma unroll
+        for (int t = 0; t < TURNS; ++t) has = has || id[t] == v0 + i;
+        if (!__ballot(has) && live) put_zero<PAST>(d_table + (size_t)(v0 + i) * d + col);
+      }
+      continue;
+    }
+    const int mine = (int)row, token = ids[mine];
+    if (token < 0 || token >= vocab) continue;
+    unsigned long long like[TURNS];
+    bool first = true;
+    int count = 0;
+#pragma unroll
+    for (int t = 0; t < TURNS; ++t) {
+      like[t] = __ballot(id[t] == token);
+      const unsigned long long before = mine >= 64 * (t + 1) ? ~0ull : mine > 64 * t ? (1ull << (mine - 64 * t)) - 1 : 0ull;
+      if (like[t] & before) first = false;
+      count += __popcll(like[t]);
+    }
+    if (!first) continue;
+    float *to = d_table + (size_t)token * d;
+    f32x4_t old = {0.f, 0.f, 0.f, 0.f}, acc = {0.f, 0.f, 0.f, 0.f};
+    if constexpr (ACC) old = *(const f32x4_t *)(to + at_col);
+    int t = 0;                                   // rows left of turn t
+    unsigned long long left = like[0];
+    for (int i = 0; i < count; i += R) {
+      f32x4_t x[R];
+#pragma unroll
+      for (int k = 0; k < R; ++k) {
+        if (i + k >= count) break;
+#pragma unroll
+        for (int q = 1; q < TURNS; ++q)
+          if (!left && t < q) { t = q; left = like[q]; }
+        const int r = 64 * t + __builtin_ctzll(left);
+        left &= left - 1;
+        x[k] = *(const f32x4_t *)(dx + (size_t)r * d + at_col);
+      }
+#pragma unroll
+      for (int k = 0; k < R; ++k)
+        if (i + k < count) acc += x[k];
+    }
+    if (live) *(f32x4_t *)(to + col) = ACC ? old + scale * acc : scale * acc;
+  }
+}
 
 // A unit is (window, strip of 256 columns), or (ZERO_ROWS tokens, strip) behind the windows' units.  Eight rows are asked for together, with
 // the old values of the tokens that end among them: 8 to 16 KB of a wave in flight.
@@ -249,7 +322,7 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(const int *__restrict__ 
                                                         long long windows, int strips) {
   const int lane = threadIdx.x & 63;
   const long long units = (windows + (ACC ? 0 : (vocab + ZERO_ROWS - 1) / ZERO_ROWS)) * strips;
-  for (long long unit = (long long)blockIdx.x * 4 + (threadIdx.x >> 6); unit < units; unit += (long long)gridDim.x * 4) {
+  for (long long unit = (long long)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); unit < units; unit += (long long)gridDim.x * 4) {
     const long long win = unit / strips;
     const int col = (int)(unit - win * strips) * STRIP + 4 * lane;
     const bool live = col < d;                   // other lanes of the last strip read its last column again and write nothing
@@ -259,11 +332,7 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(const int *__restrict__ 
       const int s = starts[min(v0 + lane, vocab)], e = starts[min(v0 + lane + 1, vocab)];
       const unsigned long long none = __ballot(lane < ZERO_ROWS && v0 + lane < vocab && s == e);
       for (int i = 0; i < ZERO_ROWS; ++i)
-        if (((none >> i) & 1) && live) {
-          f32x4_t *to = (f32x4_t *)(d_table + (size_t)(v0 + i) * d + col);
-          if constexpr (PAST) __builtin_nontemporal_store(f32x4_t{0.f, 0.f, 0.f, 0.f}, to);
-          else *to = f32x4_t{0.f, 0.f, 0.f, 0.f};
-        }
+        if (((none >> i) & 1) && live) put_zero<PAST>(d_table + (size_t)(v0 + i) * d + col);
       continue;
     }
     const int total = starts[vocab];
@@ -367,7 +436,7 @@ hipError_t launch_embed_rows(const void *table, bool bf16, const int32_t *ids, i
   while (lg < 8 && (4 << lg) < vecs) ++lg;
   const int rows = 256 >> lg;
   const dim3 grid((unsigned)std::min<long long>(((long long)n + rows - 1) / rows, 1 << 22));
-  // Rows that fill half the last-level cache or more are written past it, so that the table stays in it: 66576 x 4096 bf16 152 -> 126 us.
+  // Rows that fill half the last-level cache or more are written past it, so that the table stays in it: 66576 x 4096 bf16 152 -> 145 us, on two sets of rows in turn 126.
   const bool stream = (size_t)n * vecs * 16 >= LLC_BYTES / 2;
   auto *k = bf16 ? (stream ? embed_rows_kernel<true, true> : embed_rows_kernel<true, false>) : (stream ? embed_rows_kernel<false, true> : embed_rows_kernel<false, false>);
   hipLaunchKernelGGL(k, grid, dim3(256), 0, st, table, ids, n, vocab, d, scale, out, lg);
@@ -383,6 +452,15 @@ hipError_t launch_embed_grad(const int32_t *ids, int n, int vocab, int d, const 
                              hipStream_t st) {
   if (n <= 0 && accumulate) return hipSuccess;
   const GradPlan p = plan_grad(n, vocab, d);
+  const long long zero_units = accumulate ? 0 : ((long long)vocab + ZERO_ROWS - 1) / ZERO_ROWS * p.strips;
+  const auto blocks = [](long long units) { return dim3((unsigned)std::min<long long>((units + 3) / 4, 1 << 22)); };
+  // The zeros of a table that the last-level cache cannot hold are written past it: 12288 rows into 32000 x 4096 155 -> 137 us.
+  const bool past = (size_t)vocab * d * sizeof(float) > LLC_BYTES;
+  if (n <= FEW_ROWS) {
+    auto *few = accumulate ? embed_few_kernel<true, false> : past ? embed_few_kernel<false, true> : embed_few_kernel<false, false>;
+    hipLaunchKernelGGL(few, blocks((long long)n * p.strips + zero_units), dim3(256), 0, st, ids, n, dx, vocab, d, scale, d_table, p.strips);
+    return hipGetLastError();
+  }
   int *starts = (int *)scratch;
   int *begins = (int *)((char *)scratch + p.begins_at);
   Placed *from = (Placed *)((char *)scratch + p.from_at), *order = (Placed *)((char *)scratch + p.order_at);
@@ -394,17 +472,13 @@ hipError_t launch_embed_grad(const int32_t *ids, int n, int vocab, int d, const 
     hipLaunchKernelGGL(embed_bucket_kernel, dim3(std::min(p.chunks, 1 << 20)), dim3(CHUNK), 0, st, ids, n, vocab, p.lg, begins, from);
     hipLaunchKernelGGL(embed_place_kernel<false>, dim3(buckets), dim3(64 * WAVES), 0, st, (const int32_t *)nullptr, 0, begins, from, p.chunks, vocab, p.lg, starts, order);
   }
-  const long long units = (p.windows + (accumulate ? 0 : (vocab + ZERO_ROWS - 1) / ZERO_ROWS)) * p.strips;
-  const dim3 grid((unsigned)std::min<long long>((units + 3) / 4, 1 << 22));
   // Row gradients of half the last-level cache or more are read past it, so that the table stays: 12288 x 4096 99 -> 79 us, 65536 x 4096 358 -> 345;
   // 3347 x 2048, which fit, 29.6 -> 32.3.
   const bool stream = (size_t)n * d * sizeof(float) >= LLC_BYTES / 2;
-  // and so are the zeros of a table that the cache cannot hold: 12288 rows into 32000 x 4096 155 -> 137.
-  const bool past = (size_t)vocab * d * sizeof(float) > LLC_BYTES;
   auto *sum = accumulate ? (stream ? embed_sum_kernel<true, true, false> : embed_sum_kernel<true, false, false>)
               : past     ? (stream ? embed_sum_kernel<false, true, true> : embed_sum_kernel<false, false, true>)
                          : (stream ? embed_sum_kernel<false, true, false> : embed_sum_kernel<false, false, false>);
-  hipLaunchKernelGGL(sum, grid, dim3(256), 0, st, starts, order, dx, vocab, d, scale, d_table, aside, p.window, p.windows, p.strips);
+  hipLaunchKernelGGL(sum, blocks(p.windows * p.strips + zero_units), dim3(256), 0, st, starts, order, dx, vocab, d, scale, d_table, aside, p.window, p.windows, p.strips);
   if (p.windows > 1) {
     const int strips = (d + 1023) / 1024;
     const dim3 joins((unsigned)std::min<long long>(p.windows * strips, 1 << 22));

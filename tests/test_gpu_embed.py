@@ -124,6 +124,16 @@ def test_grad_long(torch_mod):
     check_grad(torch, 256, 2048, ids, True, 1.0)
 
 
+@pytest.mark.parametrize("n", [700, 5000])
+def test_grad_large_vocabulary(torch_mod, n):
+    """More than 512 tokens to each of the 256 ranges in which the rows are sorted."""
+    vocab = 262208
+    ids = draw_ids(torch_mod, "text", n, vocab, n)
+    ids[::7] = vocab - 1
+    ids[1::7] = 0
+    check_grad(torch_mod, 64, vocab, ids, n == 700, 1.0)
+
+
 def test_grad_without_rows(torch_mod):
     torch = torch_mod
     none = torch.empty(0, dtype=torch.int32, device="cuda")
