@@ -175,7 +175,7 @@ template <bool DIRECT>
 __global__ __launch_bounds__(64 * WAVES) void embed_place_kernel(const int32_t *__restrict__ ids, int n, const int *__restrict__ begins,
                                                                  const Placed *__restrict__ from, int chunks, int vocab, int lg, int *__restrict__ starts,
                                                                  Placed *__restrict__ order) {
-  __shared__ int count[WAVES][MAX_KEYS];
+  __shared__ int count[WAVES * MAX_KEYS];        // [wave][key]
   __shared__ int red[WAVES], lower[WAVES], after;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, keys = min(1 << lg, MAX_KEYS), bits = min(lg, 9), bucket = blockIdx.x;
   const int items = DIRECT ? n : chunks, per = DIRECT ? (n + CHUNK - 1) / CHUNK * 64 : (chunks + WAVES - 1) / WAVES;
@@ -191,10 +191,10 @@ __global__ __launch_bounds__(64 * WAVES) void embed_place_kernel(const int32_t *
   int here = 0;                                  // where this turn's tokens begin
   for (long long v0 = begin; v0 < end; v0 += MAX_KEYS) {       // (one turn for vocabularies of up to 131072)
     const int first = (int)v0, last = (int)min(end, v0 + keys);
-    for (int k = threadIdx.x; k < WAVES * MAX_KEYS; k += 64 * WAVES) (&count[0][0])[k] = 0;
+    for (int k = threadIdx.x; k < WAVES * keys; k += 64 * WAVES) count[k] = 0;
     __syncthreads();
     rows([&](Placed p, bool in) {
-      if (in && p.token >= first && p.token < last) atomicAdd(&count[wave][p.token - first], 1);
+      if (in && p.token >= first && p.token < last) atomicAdd(&count[wave * keys + p.token - first], 1);
       if (DIRECT && v0 == begin && p.token >= 0 && p.token < first) ++below;
     });
     if (v0 == begin) {
@@ -209,15 +209,15 @@ __global__ __launch_bounds__(64 * WAVES) void embed_place_kernel(const int32_t *
     int mine = 0;
     if (threadIdx.x < keys)
 #pragma unroll
-      for (int w = 0; w < WAVES; ++w) mine += count[w][threadIdx.x];
+      for (int w = 0; w < WAVES; ++w) mine += count[w * keys + threadIdx.x];
     int at = sum_before(mine, red) + here;
     if (threadIdx.x < keys) {
       if (first + (int)threadIdx.x < last) starts[first + threadIdx.x] = at;
       if (first + (int)threadIdx.x == vocab - 1) starts[vocab] = at + mine;
 #pragma unroll
       for (int w = 0; w < WAVES; ++w) {
-        const int x = count[w][threadIdx.x];
-        count[w][threadIdx.x] = at;
+        const int x = count[w * keys + threadIdx.x];
+        count[w * keys + threadIdx.x] = at;
         at += x;
       }
       if (threadIdx.x == keys - 1) after = at;
@@ -231,7 +231,7 @@ __global__ __launch_bounds__(64 * WAVES) void embed_place_kernel(const int32_t *
       const unsigned long long same = lanes_like(key, bits, in);
       const int leader = in ? __builtin_ctzll(same) : lane;
       int to = 0;
-      if (in && lane == leader) to = atomicAdd(&count[wave][key], __popcll(same));      // only this wave's lanes, one turn after the other
+      if (in && lane == leader) to = atomicAdd(&count[wave * keys + key], __popcll(same));      // only this wave's lanes, one turn after the other
       to = __shfl(to, leader, 64) + lower_lanes(same);
       if (in) order[to] = p;
     });
@@ -248,14 +248,14 @@ __device__ __forceinline__ void put_zero(float *to) {
   else *(f32x4_t *)to = z;
 }
 
-// The whole gradient of at most FEW_ROWS rows in one launch instead of three (us, 32 rows of 4096 9.8 -> 3.5, 256 rows 11.7 -> 4.7; 256 rows of one
+// The whole gradient of at most ROWS rows in one launch instead of three (us, 32 rows of 4096 9.8 -> 3.5, 256 rows 11.7 -> 4.7; 256 rows of one
 // token, the longest sum, 16.9 -> 29.7).  A unit is (row, strip of 256 columns): the first row of a token sums all of them, by looking
 // through the ids; or (ZERO_ROWS tokens, strip) behind the rows' units.
-constexpr int FEW_ROWS = 256;
+constexpr int ROWS = 256;
 template <bool ACC, bool PAST>
 __global__ __launch_bounds__(256) void embed_few_kernel(const int32_t *__restrict__ ids, int n, const float *__restrict__ dx, int vocab, int d, float scale,
                                                         float *__restrict__ d_table, int strips) {
-  constexpr int TURNS = FEW_ROWS / 64;
+  constexpr int TURNS = ROWS / 64;
   const int lane = threadIdx.x & 63;
   const long long units = (n + (ACC ? 0 : ((long long)vocab + ZERO_ROWS - 1) / ZERO_ROWS)) * strips;
   int id[TURNS];
@@ -388,12 +388,12 @@ __global__ __launch_bounds__(256) void embed_join_kernel(const int *__restrict__
     const long long last = (e - 1) / window;
     f32x4_t acc = *(const f32x4_t *)(aside + (size_t)(2 * win + 1) * d + col), old = {0.f, 0.f, 0.f, 0.f};
     if constexpr (ACC) old = *(const f32x4_t *)(d_table + (size_t)token * d + col);
-    for (long long w = win + 1; w <= last; w += 8) {
-      f32x4_t x[8];
+    for (long long w = win + 1; w <= last; w += 16) {
+      f32x4_t x[16];
 #pragma unroll
-      for (int k = 0; k < 8; ++k) x[k] = *(const f32x4_t *)(aside + (size_t)(2 * min(w + k, last)) * d + col);
+      for (int k = 0; k < 16; ++k) x[k] = *(const f32x4_t *)(aside + (size_t)(2 * min(w + k, last)) * d + col);
 #pragma unroll
-      for (int k = 0; k < 8; ++k)
+      for (int k = 0; k < 16; ++k)
         if (w + k <= last) acc += x[k];
     }
     *(f32x4_t *)(d_table + (size_t)token * d + col) = ACC ? old + scale * acc : scale * acc;
@@ -456,7 +456,7 @@ hipError_t launch_embed_grad(const int32_t *ids, int n, int vocab, int d, const 
   const auto blocks = [](long long units) { return dim3((unsigned)std::min<long long>((units + 3) / 4, 1 << 22)); };
   // The zeros of a table that the last-level cache cannot hold are written past it: 12288 rows into 32000 x 4096 155 -> 137 us.
   const bool past = (size_t)vocab * d * sizeof(float) > LLC_BYTES;
-  if (n <= FEW_ROWS) {
+  if (n <= ROWS) {
     auto *few = accumulate ? embed_few_kernel<true, false> : past ? embed_few_kernel<false, true> : embed_few_kernel<false, false>;
     hipLaunchKernelGGL(few, blocks((long long)n * p.strips + zero_units), dim3(256), 0, st, ids, n, dx, vocab, d, scale, d_table, p.strips);
     return hipGetLastError();
