@@ -402,7 +402,7 @@ def _workspace(h, t):
 def mace_embed_tokens(h, table, token_ids, out, scale: float = 1.0, stream=None):
     """out[r] = scale * table[token_ids[r]]; table [vocab, d_model] and out [n, d_model] in the handle's type."""
     n = token_ids.shape[0]
-    _check(load().mace_embed_tokens(h, _tensor(h, table, "table", h.io_dtype, h.table_shape), _tensor(h, token_ids, "token_ids", torch.int32, (n,)), n, scale,
+    _check(load().mace_embed_tokens(h, _tensor(h, table, "table", h.io_dtype, h.table_shape), _tensor(h, token_ids, "token_ids", torch.int32, (n,)), n, float(scale),
                                     _tensor(h, out, "out", h.io_dtype, (n, h.table_shape[1])), _stream(stream)), "mace_embed_tokens")
 
 
@@ -414,7 +414,7 @@ def mace_embed_tokens_grad(h, token_ids, dx, d_table, workspace, scale: float = 
     """d_table[v] (+)= scale * sum of dx[r] over the rows with token_ids[r] == v; dx [n, d_model], d_table [vocab, d_model] fp32."""
     n = token_ids.shape[0]
     _check(load().mace_embed_tokens_grad(h, _tensor(h, token_ids, "token_ids", torch.int32, (n,)), n,
-                                         _tensor(h, dx, "dx", torch.float32, (n, h.table_shape[1])), scale,
+                                         _tensor(h, dx, "dx", torch.float32, (n, h.table_shape[1])), float(scale),
                                          _tensor(h, d_table, "d_table", torch.float32, h.table_shape), int(accumulate), *_workspace(h, workspace),
                                          _stream(stream)), "mace_embed_tokens_grad")
 

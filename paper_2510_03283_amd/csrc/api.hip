@@ -936,7 +936,13 @@ int mace_token_logprobs(mace_handle_t h, const void *logits, int32_t dtype, int3
   if (logp && !token_ids) return fail(MACE_INVALID_ARG, "mace_token_logprobs: logp needs token_ids");
   if (top_k > 0 ? !top_ids : top_ids || top_logp) return fail(MACE_INVALID_ARG, "mace_token_logprobs: top_k needs top_ids, and top_ids or top_logp need top_k");
   if (((uintptr_t)token_ids | (uintptr_t)logp | (uintptr_t)entropy | (uintptr_t)row_stats | (uintptr_t)top_ids | (uintptr_t)top_logp) & 3) return fail(MACE_INVALID_ARG, "mace_token_logprobs: pointer not aligned to its elements");
-  TRY(check_scratch(workspace, workspace_bytes, mace_token_logprobs_workspace_bytes(h, n, vocab, top_k), what));
+  const size_t need = mace_token_logprobs_workspace_bytes(h, n, vocab, top_k);
+  TRY(check_scratch(workspace, workspace_bytes, need, what));
+  const struct { const void *p; size_t bytes; } written[] = {{logp, (size_t)4 * n}, {entropy, (size_t)4 * n}, {row_stats, (size_t)8 * n},
+                                                             {top_ids, (size_t)4 * n * top_k}, {top_logp, (size_t)4 * n * top_k}, {workspace, need}};
+  for (const auto &r : written)
+    if (r.p && (overlap(r.p, r.bytes, logits, rows_bytes(n, vocab, ld, dtype)) || (token_ids && overlap(r.p, r.bytes, token_ids, (size_t)4 * n))))
+      return fail(MACE_INVALID_ARG, "mace_token_logprobs: an output or the workspace overlaps an input");
   TRY(check_device(h, what));
   const TokenLogprobs a = {logits, ld, n, vocab, top_k, token_ids, logp, entropy, row_stats, top_logp, top_ids};
   prof_mark(h, (hipStream_t)stream, T_LOGSOFTMAX);

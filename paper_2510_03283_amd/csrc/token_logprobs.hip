@@ -61,6 +61,11 @@ __device__ __forceinline__ float reference_of(float m) {
 #pragma clang fp contract(off)
   return fmaxf(m, -BIG) * LOG2E;
 }
+// u - delta s, the product rounded as the sum's own terms are: a row with one allowed token has an entropy of exactly 0.
+__device__ __forceinline__ float without(float u, float delta, float s) {
+#pragma clang fp contract(off)
+  return u - delta * s;
+}
 __device__ __forceinline__ float exp_of(float t) { return __builtin_amdgcn_exp2f(t * LOG2E); }
 
 // Reductions over a wave without LDS: quads, halves and rows of 16 lanes by DPP, the four rows through scalar registers.
@@ -121,7 +126,7 @@ __device__ __forceinline__ Row finish(const State &t, const TokenLogprobs &a, si
       a.row_stats[2 * r] = o.m;
       a.row_stats[2 * r + 1] = o.L;
     }
-    if (a.entropy) a.entropy[r] = o.empty ? 0.f : o.L - t.u * __builtin_amdgcn_rcpf(s);
+    if (a.entropy) a.entropy[r] = o.bad ? NAN : o.empty ? 0.f : fmaxf(o.L - t.u * __builtin_amdgcn_rcpf(s), 0.f);
     if (a.logp) a.logp[r] = given ? o.logp(x_token) : 0.f;
   }
   return o;
@@ -396,7 +401,7 @@ __global__ __launch_bounds__(NT, NT == 64 ? 5 : 1) void token_logprobs_kernel(co
       const float delta = fmaf(m, LOG2E, -m2), e0 = __builtin_amdgcn_exp2f(delta);
       one = s > 0.f && e0 > 0.f;
       const float inv = __builtin_amdgcn_rcpf(e0);
-      u = one ? (u - delta * s) * (LN2 * inv) : 0.f;
+      u = one ? without(u, delta, s) * (LN2 * inv) : 0.f;
       s = one ? (s - e0) * inv : s;
     } else {                                     // a maximum of huge magnitude: again, with differences of the logits themselves
       top = st.m;

@@ -82,6 +82,23 @@ def test_rows_copy_infinities_and_nan(torch_mod):
     assert (got[[1, 4, 5]] == 0).all()                                      # padding is zero, whatever the table holds
 
 
+@pytest.mark.parametrize("bf16", [True, False])
+def test_rows_unscaled_are_copies(torch_mod, bf16):
+    """Every finite bit pattern of bf16, subnormal numbers and both zeros among them, and as many of fp32."""
+    torch = torch_mod
+    bits = torch.arange(65536, dtype=torch.int32, device="cuda")
+    bits = bits[(bits & 0x7F80) != 0x7F80]
+    bits = torch.cat([bits, bits[:(-len(bits)) % (64 * 64)]]).view(-1, 64)
+    table = bits.to(torch.int16).view(torch.bfloat16) if bf16 else ((bits << 16) | (bits * 40503 & 0xFFFF)).view(torch.float32)
+    n = table.shape[0]
+    out = torch.empty_like(table)
+    with Model(64, n, bf16) as (B, h):
+        B.mace_embed_tokens(h, table, torch.arange(n, dtype=torch.int32, device="cuda"), out)
+        torch.cuda.synchronize()
+    kind = torch.int16 if bf16 else torch.int32
+    assert torch.equal(out.view(kind), table.view(kind))
+
+
 def check_grad(torch, d, vocab, ids, accumulate, scale, seed=0):
     n = ids.numel()
     gen = torch.Generator(device="cuda").manual_seed(seed)

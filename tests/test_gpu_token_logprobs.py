@@ -152,6 +152,38 @@ def test_values(torch_mod, lib, dtype, kind, n, vocab, k):
     check(torch, rows, token, o, k)
 
 
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("n,vocab", [(8, 130), (8, 5000), (2100, 700), (8, 131072)])
+def test_magnitudes(torch_mod, lib, dtype, n, vocab):
+    """Logits around every magnitude, one to a row, up to the largest; differences of a few there where the type has them."""
+    torch = torch_mod
+    x, token = draw(torch, n, vocab, "plain", 5)
+    centre = torch.tensor([0.0, 9.0e5, -9.0e5, 2.0e6, -2.0e6, 1e30, -1e30, 3e38], device="cuda").repeat(n // 8 + 1)[:n, None]
+    x = x + centre
+    x[1::8, ::3] = LOWEST                                                    # far below the rest, but allowed
+    x[2::8, ::3] = -INF
+    rows = rows_of(torch, x, vocab, 0, dtype)
+    o = call(torch, lib, rows, token, 6)
+    torch.cuda.synchronize()
+    check(torch, rows, token, o, 6)
+
+
+@pytest.mark.parametrize("rest", [-INF, LOWEST])
+def test_one_allowed_token_in_a_long_row(torch_mod, lib, rest):
+    """Rows that several blocks share, with everything in one of them."""
+    torch = torch_mod
+    n, vocab = 5, 128011
+    x = torch.full((n, vocab), rest, device="cuda")
+    at = torch.tensor([0, 40000, 65535, 100000, vocab - 1], device="cuda")
+    x[torch.arange(n), at] = torch.tensor([1.0, -3.0, 0.0, 30.0, -200.0], device="cuda")
+    token = at.int()
+    token[2] = 7
+    o = call(torch, lib, x, token, 4)
+    torch.cuda.synchronize()
+    check(torch, x, token, o, 4)
+    assert torch.equal(o["top_ids"][:, 0].long(), at) and (o["entropy"] == 0).all()
+
+
 def test_very_long_rows(torch_mod, lib):
     torch = torch_mod
     for n, vocab, dtype in ((3, 1 << 22, "fp32"), (600, 300001, "bf16")):
@@ -197,7 +229,7 @@ def test_only_the_vocabulary_counts(torch_mod, lib):
 
 
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
-@pytest.mark.parametrize("vocab", [5, 2048, 40001])
+@pytest.mark.parametrize("vocab", [5, 2048, 40001, 128011])
 def test_nan_and_infinity(torch_mod, lib, dtype, vocab):
     """A NaN or +inf makes its own row NaN and no other."""
     torch = torch_mod

@@ -47,6 +47,8 @@ REFUSED = [
     ("logprobs", dict(ld=1 << 31), SHAPE), ("logprobs", dict(top_k=33), SHAPE), ("logprobs", dict(top_k=-1), SHAPE),
     ("logprobs", dict(top_k=5, null="top_ids"), INVALID), ("logprobs", dict(top_k=0, top=1), INVALID), ("logprobs", dict(misalign="logits"), INVALID),
     ("logprobs", dict(misalign="logits", by=1, dtype=1), INVALID), ("logprobs", dict(misalign="logp"), INVALID), ("logprobs", dict(misalign="work", by=64), INVALID),
+    ("logprobs", dict(same="logits,stats"), INVALID), ("logprobs", dict(same="logits,top_logp", top_k=3), INVALID), ("logprobs", dict(same="logits,work"), INVALID),
+    ("logprobs", dict(same="ids,logp"), INVALID),
     ("logprobs", dict(work=0), SMALL), ("logprobs", dict(n=1, vocab=32000, top_k=5, work=0), SMALL), ("logprobs", dict(device=1), INVALID),
     ("logprobs_grad", dict(null="handle"), INVALID), ("logprobs_grad", dict(null="logits"), INVALID), ("logprobs_grad", dict(null="stats"), INVALID),
     ("logprobs_grad", dict(null="ids"), INVALID), ("logprobs_grad", dict(null="entropy"), INVALID), ("logprobs_grad", dict(null="d_logits"), INVALID),
