@@ -248,14 +248,14 @@ __device__ __forceinline__ void put_zero(float *to) {
   else *(f32x4_t *)to = z;
 }
 
-// The whole gradient of at most ROWS rows in one launch instead of three (us, 32 rows of 4096 9.8 -> 3.5, 256 rows 11.7 -> 4.7; 256 rows of one
+// The whole gradient of at most FEW_ROWS rows in one launch instead of three (us, 32 rows of 4096 9.8 -> 3.5, 256 rows 11.7 -> 4.7; 256 rows of one
 // token, the longest sum, 16.9 -> 29.7).  A unit is (row, strip of 256 columns): the first row of a token sums all of them, by looking
 // through the ids; or (ZERO_ROWS tokens, strip) behind the rows' units.
-constexpr int ROWS = 256;
+constexpr int FEW_ROWS = 256;
 template <bool ACC, bool PAST>
 __global__ __launch_bounds__(256) void embed_few_kernel(const int32_t *__restrict__ ids, int n, const float *__restrict__ dx, int vocab, int d, float scale,
                                                         float *__restrict__ d_table, int strips) {
-  constexpr int TURNS = ROWS / 64;
+  constexpr int TURNS = FEW_ROWS / 64;
   const int lane = threadIdx.x & 63;
   const long long units = (n + (ACC ? 0 : ((long long)vocab + ZERO_ROWS - 1) / ZERO_ROWS)) * strips;
   int id[TURNS];
@@ -412,7 +412,7 @@ GradPlan plan_grad(int n, int vocab, int d) {
   GradPlan p;
   p.strips = (d + STRIP - 1) / STRIP;
   p.window = 64;
-  while (p.window > 4 && (long long)((n + p.window - 1) / p.window) * p.strips < UNITS) p.window >>= 1;
+  while (p.window > 4 && ((long long)n + p.window - 1) / p.window * p.strips < UNITS) p.window >>= 1;
   p.windows = ((long long)n + p.window - 1) / p.window;
   p.lg = 0;
   while (((long long)vocab - 1) >> p.lg >= BUCKETS) ++p.lg;
@@ -456,7 +456,7 @@ hipError_t launch_embed_grad(const int32_t *ids, int n, int vocab, int d, const 
   const auto blocks = [](long long units) { return dim3((unsigned)std::min<long long>((units + 3) / 4, 1 << 22)); };
   // The zeros of a table that the last-level cache cannot hold are written past it: 12288 rows into 32000 x 4096 155 -> 137 us.
   const bool past = (size_t)vocab * d * sizeof(float) > LLC_BYTES;
-  if (n <= ROWS) {
+  if (n <= FEW_ROWS) {
     auto *few = accumulate ? embed_few_kernel<true, false> : past ? embed_few_kernel<false, true> : embed_few_kernel<false, false>;
     hipLaunchKernelGGL(few, blocks((long long)n * p.strips + zero_units), dim3(256), 0, st, ids, n, dx, vocab, d, scale, d_table, p.strips);
     return hipGetLastError();

@@ -399,7 +399,7 @@ __global__ __launch_bounds__(NT, NT == 64 ? 5 : 1) void token_logprobs_kernel(co
     bool one;
     if (fabsf(st.m) <= BIG || st.m == -INFINITY) {          // (-inf: nothing but banned tokens, no term is there)
       const float delta = fmaf(m, LOG2E, -m2), e0 = __builtin_amdgcn_exp2f(delta);
-      one = s > 0.f && e0 > 0.f;
+      one = s > 0.f && e0 > 1e-30f;
       const float inv = __builtin_amdgcn_rcpf(e0);
       u = one ? without(u, delta, s) * (LN2 * inv) : 0.f;
       s = one ? (s - e0) * inv : s;
