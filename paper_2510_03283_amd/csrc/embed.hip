@@ -47,8 +47,8 @@ __global__ __launch_bounds__(256) void embed_rows_kernel(const void *__restrict_
 }
 
 // ------------------------------------------------------------------ gradient of the table
-// Four launches, no block of which waits for another, and no order of which depends on which block comes first.
-//  bucket The ids are cut into chunks of 1024 rows; a block sorts its chunk by bucket, 2^lg adjacent tokens (stable: rows of a bucket
+// Two to four launches (one for few rows), no block of which waits for another, and no order of which depends on which block comes first.
+//  bucket (many rows only) The ids are cut into chunks of 1024 rows; a block sorts its chunk by bucket, 2^lg adjacent tokens (stable: rows of a bucket
 //         keep their order), and notes how many rows each bucket has in it.
 //  place  A block per bucket collects the bucket's rows from all chunks in order and sorts them by token, again stably.  The rows of
 //         lower buckets, counted over the chunks, say where the bucket begins.
@@ -157,32 +157,29 @@ __device__ __forceinline__ void bucket_rows(const Placed *from, const int *begin
   }
 }
 
-// From the ids c0 .. c1 themselves; the caller looks which of them are its bucket's.
-template <typename F>
-__device__ __forceinline__ void bucket_rows(const int32_t *ids, int c0, int c1, F f) {
-  const int lane = threadIdx.x & 63;
-  for (int i0 = c0; i0 < c1; i0 += 4 * 64) {
-    int id[4];
-#pragma unroll
-    for (int k = 0; k < 4; ++k) id[k] = i0 + 64 * k + lane < c1 ? ids[i0 + 64 * k + lane] : -1;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) f(Placed{i0 + 64 * k + lane, id[k]}, true);
-  }
-}
-
-// starts[v]: rows of tokens below v, v = 0 .. vocab; order: the rows by token.  DIRECT: from n ids instead of sorted chunks.
-template <bool DIRECT>
+// starts[v]: rows of tokens below v, v = 0 .. vocab; order: the rows by token.  From sorted chunks or, IDS > 0, from the n <= IDS * CHUNK ids
+// themselves: every block looks through all of them, IDS a thread and read once, which saves the bucket kernel.
+template <int IDS>
 __global__ __launch_bounds__(64 * WAVES) void embed_place_kernel(const int32_t *__restrict__ ids, int n, const int *__restrict__ begins,
                                                                  const Placed *__restrict__ from, int chunks, int vocab, int lg, int *__restrict__ starts,
                                                                  Placed *__restrict__ order) {
   __shared__ int count[WAVES * MAX_KEYS];        // [wave][key]
   __shared__ int red[WAVES], lower[WAVES], after;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, keys = min(1 << lg, MAX_KEYS), bits = min(lg, 9), bucket = blockIdx.x;
-  const int items = DIRECT ? n : chunks, per = DIRECT ? (n + CHUNK - 1) / CHUNK * 64 : (chunks + WAVES - 1) / WAVES;
-  const int c0 = min(items, per * wave), c1 = min(items, c0 + per);
+  constexpr bool DIRECT = IDS > 0;
+  const int per = DIRECT ? (n + CHUNK - 1) / CHUNK * 64 : (chunks + WAVES - 1) / WAVES;      // ids, chunks of a wave
+  const int c0 = min(DIRECT ? n : chunks, per * wave), c1 = min(DIRECT ? n : chunks, c0 + per);
+  int id[DIRECT ? IDS : 1];
+  if constexpr (DIRECT)
+#pragma unroll
+    for (int k = 0; k < IDS; ++k) id[k] = c0 + 64 * k + lane < c1 ? ids[c0 + 64 * k + lane] : -1;
   const auto rows = [&](auto f) {
-    if constexpr (DIRECT) bucket_rows(ids, c0, c1, f);
-    else bucket_rows(from, begins, bucket, c0, c1, f);
+    if constexpr (DIRECT) {
+#pragma unroll
+      for (int k = 0; k < IDS; ++k) f(Placed{c0 + 64 * k + lane, id[k]}, true);
+    } else {
+      bucket_rows(from, begins, bucket, c0, c1, f);
+    }
   };
   const long long begin = (long long)bucket << lg, end = min((long long)vocab, begin + (1ll << lg));
   int below = 0;                                 // rows of lower buckets
@@ -445,9 +442,6 @@ hipError_t launch_embed_rows(const void *table, bool bf16, const int32_t *ids, i
 
 size_t embed_grad_scratch_bytes(int n, int vocab, int d) { return plan_grad(n, vocab, d).bytes; }
 
-// Up to so many rows every block of the place kernel looks through all ids, which saves the bucket kernel (us in all: 64 x 4096 18.3 -> 14.0, 3347 x 2048 52.5
-// -> 49.9, 6000 x 1024 no difference, 8192 x 1024 42.8 -> 44.9).
-constexpr int DIRECT_ROWS = 4096;
 hipError_t launch_embed_grad(const int32_t *ids, int n, int vocab, int d, const float *dx, float scale, float *d_table, bool accumulate, void *scratch,
                              hipStream_t st) {
   if (n <= 0 && accumulate) return hipSuccess;
@@ -466,11 +460,14 @@ hipError_t launch_embed_grad(const int32_t *ids, int n, int vocab, int d, const 
   Placed *from = (Placed *)((char *)scratch + p.from_at), *order = (Placed *)((char *)scratch + p.order_at);
   float *aside = (float *)((char *)scratch + p.aside_at);
   const int buckets = ((vocab - 1) >> p.lg) + 1;
-  if (n <= DIRECT_ROWS) {
-    hipLaunchKernelGGL(embed_place_kernel<true>, dim3(buckets), dim3(64 * WAVES), 0, st, ids, n, (const int *)nullptr, (const Placed *)nullptr, 0, vocab, p.lg, starts, order);
+  // us in all with the bucket kernel / four / eight / sixteen ids a thread: 300 x 4096 18.1 / 13.5 / 14.1 / 15.2, 3347 x 2048 26.6 / 23.0 / 23.7 / 24.7,
+  // 6000 x 1024 26.1 / - / 23.5 / 25.2, 8192 x 1024 27.6 / - / 26.7 / 27.9, 16384 x 1024 40.0 / - / - / 43.4.
+  if (n <= 8 * CHUNK) {
+    hipLaunchKernelGGL(n <= 4 * CHUNK ? embed_place_kernel<4> : embed_place_kernel<8>, dim3(buckets), dim3(64 * WAVES), 0, st, ids, n, (const int *)nullptr,
+                       (const Placed *)nullptr, 0, vocab, p.lg, starts, order);
   } else {
     hipLaunchKernelGGL(embed_bucket_kernel, dim3(std::min(p.chunks, 1 << 20)), dim3(CHUNK), 0, st, ids, n, vocab, p.lg, begins, from);
-    hipLaunchKernelGGL(embed_place_kernel<false>, dim3(buckets), dim3(64 * WAVES), 0, st, (const int32_t *)nullptr, 0, begins, from, p.chunks, vocab, p.lg, starts, order);
+    hipLaunchKernelGGL(embed_place_kernel<0>, dim3(buckets), dim3(64 * WAVES), 0, st, (const int32_t *)nullptr, 0, begins, from, p.chunks, vocab, p.lg, starts, order);
   }
   // Row gradients of half the last-level cache or more are read past it, so that the table stays: 12288 x 4096 99 -> 79 us, 65536 x 4096 358 -> 345;
   // 3347 x 2048, which fit, 29.6 -> 32.3.

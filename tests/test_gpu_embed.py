@@ -128,7 +128,8 @@ def check_grad(torch, d, vocab, ids, accumulate, scale, seed=0):
 @pytest.mark.parametrize("kind,n,d,vocab", [
     ("uniform", 1, 64, 64), ("uniform", 2, 128, 32000), ("one", 63, 64, 64), ("one", 65, 192, 128), ("two", 64, 256, 2048), ("padding", 100, 64, 640),
     ("text", 257, 256, 2048), ("uniform", 1000, 2048, 32000), ("sorted", 999, 1024, 512), ("runs", 4096, 320, 2048), ("text", 3347, 2048, 32000),
-    ("one", 5000, 512, 1024), ("two", 4099, 4096, 6400), ("text", 20011, 1024, 128000), ("text", 2100, 8192, 704), ("uniform", 9000, 64, 64)])
+    ("one", 5000, 512, 1024), ("two", 4099, 4096, 6400), ("text", 20011, 1024, 128000), ("text", 2100, 8192, 704), ("uniform", 9000, 64, 64),
+    ("text", 8192, 128, 32000), ("text", 8193, 128, 200000), ("uniform", 6001, 64, 200000)])
 def test_grad(torch_mod, accumulate, kind, n, d, vocab):
     check_grad(torch_mod, d, vocab, draw_ids(torch_mod, kind, n, vocab, n), accumulate, 1.0 if n % 2 else 0.7)
 

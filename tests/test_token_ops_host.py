@@ -89,7 +89,7 @@ def test_gradient_over_its_own_logits(recorder):
 
 
 def test_workspace_of_more_rows_serves_fewer(recorder):
-    sizes = [1, 2, 3, 31, 64, 65, 100, 255, 256, 257, 511, 513, 1000, 4095, 4096, 4097, 16384, 20001, 65536, 100000]
+    sizes = [1, 2, 3, 31, 64, 65, 100, 255, 256, 257, 511, 513, 1000, 4095, 4096, 4097, 8191, 8192, 8193, 16384, 20001, 65536, 100000]
     need = [recorder("embed_grad", n=n)[3] for n in sizes]
     assert need == sorted(need)
     for vocab, k in ((100, 0), (2048, 5), (32000, 0), (32000, 20), (128011, 32), (1 << 22, 1)):
