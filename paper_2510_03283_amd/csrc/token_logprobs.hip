@@ -137,7 +137,7 @@ constexpr int RANK_STEP = 8;
 
 // A turn of a block of NT threads is NT * U consecutive 16-byte accesses; the four lanes of a quad hold U x 64 bytes of it, a group,
 // whose maximum is kept: the alternatives are then found without a second pass over the row.  MAX_GROUPS maxima fit the LDS (131072
-// fp32 columns of a part with 256 threads, 8192 with 64), and CAND candidates.
+// fp32 columns of a part with 256 or 512 threads, 8192 with 64), and CAND candidates.
 template <bool BF16, int NT>
 struct Turn {
   static constexpr int N = Chunk<BF16>::N, COLS = NT * U * N, GROUPS = NT / 4, GROUP_COLS = 4 * U * N;
@@ -300,7 +300,7 @@ __device__ __noinline__ int best_columns_crowded(TopScratch<NT> &S, const void *
 
 // The k best of columns [c0, c1): leaves at least min(k, allowed columns) of them, the best among them, in S.c and returns their
 // number.  m: this thread's maximum, -inf if it met none.
-// tau, the k-th largest of 64 maxima of disjoint sets of columns (a quad's, or a lane's), has at least k columns at or above it, and about
+// tau, the k-th largest of 64 maxima of disjoint sets of columns (a lane's, a quad's or of eight lanes), has at least k columns at or above it, and about
 // -64 log(1 - k / 64) where the values are spread by chance: 24 for k = 20, 44 for k = 32.  The groups whose maximum reaches tau, about as
 // many, are read again, 256 bytes each.
 // meanwhile: what the last wave does while the first looks for tau.
@@ -310,6 +310,7 @@ __device__ __forceinline__ int best_columns(TopScratch<NT> &S, const void *row, 
   constexpr int SET = NT / 64;                   // threads of a set
   const int n_groups = turns * T::GROUPS;
   if (SET > 1) m = max_quad(m);
+  if (SET == 8) m = fmaxf(m, dpp<HALF_MIRROR>(m));
   if (threadIdx.x % SET == 0) S.set[threadIdx.x / SET] = m;
   if (threadIdx.x == 0) S.n_list = S.n_cand = 0;
   __syncthreads();
@@ -612,7 +613,12 @@ hipError_t launch_rows(const TokenLogprobs &a, float *scratch, hipStream_t st) {
   // 30000 x 7000 146 / 152, 235 / 204; but 512 x 2048 3.9 / 4.3, 7.4 / 10.3.  64 x 500 bf16 with 20 alternatives 30.8 / 10.7.
   const int few = 128 * Turn<BF16, 256>::N;      // 32 quads with a column
   const bool wave = parts == 1 && (a.vocab <= few || (a.n >= 2048 && a.vocab <= 8192));
-  return wave ? launch_rows<BF16, 64>(a, 1, scratch, st) : launch_rows<BF16, 256>(a, parts, scratch, st);
+  if (wave) return launch_rows<BF16, 64>(a, 1, scratch, st);
+  // Blocks of 512 threads where a CU has no more than one and its turn is not much wider than the row.  us with 256 / 512 threads, 20 alternatives: one row of
+  // 32000 fp32 9.2 / 8.0, 64 10.1 / 8.8, 256 12.1 / 11.6, 320 13.5 / 14.2; one of 8000 6.7 / 6.3, without alternatives 3.6 / 3.6, of 4000 3.2 / 3.5; one of 32000
+  // bf16 9.6 / 8.3, 256 11.5 / 10.7, one of 8000 without alternatives 3.6 / 4.2.  1024 threads: 8.3 for one row of 32000, 12.6 for 256.
+  const bool wide = (long long)a.n * parts <= 256 && 4ll * a.vocab > 3 * Turn<BF16, 512>::COLS;
+  return wide ? launch_rows<BF16, 512>(a, parts, scratch, st) : launch_rows<BF16, 256>(a, parts, scratch, st);
 }
 
 }  // namespace

@@ -142,7 +142,7 @@ def test_sizes(torch_mod, lib, dtype, n, vocab):
 
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
 @pytest.mark.parametrize("kind", ["plain", "peaked", "banned", "lowest", "equal", "coarse", "rising", "falling", "large"])
-@pytest.mark.parametrize("n,vocab,k", [(12, 70, 32), (37, 2048, 20), (21, 31999, 32), (7, 131072, 8), (1100, 1003, 4)])
+@pytest.mark.parametrize("n,vocab,k", [(12, 70, 32), (37, 2048, 20), (21, 31999, 32), (7, 131072, 8), (1100, 1003, 4), (300, 12301, 20), (9, 6145, 24)])
 def test_values(torch_mod, lib, dtype, kind, n, vocab, k):
     torch = torch_mod
     x, token = draw(torch, n, vocab, kind, 11 + n)
