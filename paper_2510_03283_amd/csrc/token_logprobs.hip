@@ -331,6 +331,8 @@ __host__ __device__ __forceinline__ size_t part_floats(int k) { return (size_t)(
 // A block per row, or per part of a row.  One pass over the logits with a running maximum in every thread.  The exponent of a term is one
 // fma, x log2 e - m2, with m2 the product for the maximum rounded to fp32: every term carries the factor 2^delta,
 // delta = m log2 e - m2, which is taken out at the end (it is the term of the maximum itself).
+// 32768 x 32000 fp32: 600 us, 7.0 TB/s, HBM-bound.  2048 x 128011 bf16 with 8 alternatives: 91 us, 5.8 TB/s, bound by vector instructions (a logit takes about 9
+// slots, four of them its exponential).  One row of 32000 with 5 alternatives: 7 us, a chain of four turns, three reductions and a second look at some groups.
 template <bool BF16, bool TOP, int NT, bool STREAM>
 __global__ __launch_bounds__(NT, NT == 64 ? 5 : 1) void token_logprobs_kernel(const TokenLogprobs a, int parts, int part_turns, float *__restrict__ scratch) {
   using T = Turn<BF16, NT>;
@@ -535,7 +537,7 @@ __device__ __forceinline__ void put(char *out, size_t at, V v) {
   if constexpr (STREAM) __builtin_nontemporal_store(v, (V *)(out + at));
   else *(V *)(out + at) = v;
 }
-// A wave takes 64 x U 16-byte accesses of a row; HBM-bound, one read and one write a logit.
+// A wave takes 64 x U 16-byte accesses of a row; HBM-bound, one read and one write a logit (16384 x 32000 fp32 to bf16: 522 us, 6.0 TB/s).
 template <bool BF16, bool OUT_BF16, bool STREAM>
 __global__ __launch_bounds__(256) void token_logprobs_grad_kernel(const TokenLogprobsGrad a, int parts) {
   constexpr int N = Chunk<BF16>::N;
