@@ -341,7 +341,7 @@ int mace_embed_tokens_grad(mace_handle_t h, const int32_t *token_ids, int32_t n,
  * banned tokens: logp -inf, entropy 0, row_stats (-inf, 0).  A NaN or +inf among the vocab columns of a row: its outputs are
  * NaN (logp of padding 0) and its ids -1.  Statistics are fp32 whatever the logits' type, added in an order that depends on the sizes
  * alone.  workspace: mace_token_logprobs_workspace_bytes(h, n, vocab, top_k) bytes, 256-byte aligned, nothing of it read before it
- * is written. */
+ * is written.  Outputs and workspace overlap neither an input nor each other. */
 size_t mace_token_logprobs_workspace_bytes(mace_handle_t h, int32_t n, int32_t vocab, int32_t top_k);
 int mace_token_logprobs(mace_handle_t h, const void *logits, int32_t dtype, int32_t n, int32_t vocab, int64_t ld,
                         const int32_t *token_ids, int32_t top_k, float *logp, float *entropy, float *row_stats, int32_t *top_ids,

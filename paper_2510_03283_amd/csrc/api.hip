@@ -943,6 +943,9 @@ int mace_token_logprobs(mace_handle_t h, const void *logits, int32_t dtype, int3
   for (const auto &r : written)
     if (r.p && (overlap(r.p, r.bytes, logits, rows_bytes(n, vocab, ld, dtype)) || (token_ids && overlap(r.p, r.bytes, token_ids, (size_t)4 * n))))
       return fail(MACE_INVALID_ARG, "mace_token_logprobs: an output or the workspace overlaps an input");
+  for (const auto &r : written)
+    for (const auto *q = &r + 1; q < std::end(written); ++q)
+      if (r.p && q->p && overlap(r.p, r.bytes, q->p, q->bytes)) return fail(MACE_INVALID_ARG, "mace_token_logprobs: outputs or the workspace overlap each other");
   TRY(check_device(h, what));
   const TokenLogprobs a = {logits, ld, n, vocab, top_k, token_ids, logp, entropy, row_stats, top_logp, top_ids};
   prof_mark(h, (hipStream_t)stream, T_LOGSOFTMAX);
@@ -963,7 +966,7 @@ int mace_token_logprobs_grad(mace_handle_t h, const void *logits, int32_t dtype,
   if (d_logp && !token_ids) return fail(MACE_INVALID_ARG, "mace_token_logprobs_grad: d_logp needs token_ids");
   if (d_entropy && !entropy) return fail(MACE_INVALID_ARG, "mace_token_logprobs_grad: d_entropy needs the rows' entropy");
   if (((uintptr_t)token_ids | (uintptr_t)row_stats | (uintptr_t)entropy | (uintptr_t)d_logp | (uintptr_t)d_entropy) & 3) return fail(MACE_INVALID_ARG, "mace_token_logprobs_grad: pointer not aligned to its elements");
-  const bool in_place = logits == d_logits && dtype == d_dtype && ld == ld_d;
+  const bool in_place = logits == d_logits && dtype == d_dtype && (ld == ld_d || n == 1);
   const size_t out = rows_bytes(n, vocab, ld_d, d_dtype);
   if (!in_place && overlap(logits, rows_bytes(n, vocab, ld, dtype), d_logits, out)) return fail(MACE_INVALID_ARG, "mace_token_logprobs_grad: d_logits overlaps logits without being the same rows");
   for (const void *p : {(const void *)token_ids, (const void *)row_stats, (const void *)entropy, (const void *)d_logp, (const void *)d_entropy})

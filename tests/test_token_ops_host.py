@@ -48,7 +48,8 @@ REFUSED = [
     ("logprobs", dict(top_k=5, null="top_ids"), INVALID), ("logprobs", dict(top_k=0, top=1), INVALID), ("logprobs", dict(misalign="logits"), INVALID),
     ("logprobs", dict(misalign="logits", by=1, dtype=1), INVALID), ("logprobs", dict(misalign="logp"), INVALID), ("logprobs", dict(misalign="work", by=64), INVALID),
     ("logprobs", dict(same="logits,stats"), INVALID), ("logprobs", dict(same="logits,top_logp", top_k=3), INVALID), ("logprobs", dict(same="logits,work"), INVALID),
-    ("logprobs", dict(same="ids,logp"), INVALID),
+    ("logprobs", dict(same="ids,logp"), INVALID), ("logprobs", dict(same="logp,stats"), INVALID), ("logprobs", dict(same="entropy,work", n=1, vocab=128011), INVALID),
+    ("logprobs", dict(same="top_ids,top_logp", top_k=2), INVALID),
     ("logprobs", dict(work=0), SMALL), ("logprobs", dict(n=1, vocab=32000, top_k=5, work=0), SMALL), ("logprobs", dict(device=1), INVALID),
     ("logprobs_grad", dict(null="handle"), INVALID), ("logprobs_grad", dict(null="logits"), INVALID), ("logprobs_grad", dict(null="stats"), INVALID),
     ("logprobs_grad", dict(null="ids"), INVALID), ("logprobs_grad", dict(null="entropy"), INVALID), ("logprobs_grad", dict(null="d_logits"), INVALID),
@@ -86,6 +87,7 @@ def test_no_rows(recorder):
 def test_gradient_over_its_own_logits(recorder):
     assert recorder("logprobs_grad", same="logits,d_logits", d_dtype=0)[0] == OK
     assert recorder("logprobs_grad", same="logits,d_logits", dtype=1, d_dtype=1, ld=2056, ld_d=2056)[0] == OK
+    assert recorder("logprobs_grad", same="logits,d_logits", d_dtype=0, n=1, ld=2056)[0] == OK              # one row has no stride
 
 
 def test_workspace_of_more_rows_serves_fewer(recorder):
