@@ -326,8 +326,8 @@ int mace_embed_tokens_grad(mace_handle_t h, const int32_t *token_ids, int32_t n,
  * the best alternatives of every row: what a server reports beside a token, what a preference job needs of its reference
  * policy (the per-token terms of ref_logp, Section 3.1), what a policy-gradient step weighs.
  *   logits     device, dtype MACE_F32 or MACE_BF16, n rows of vocab columns that lie ld elements apart (ld >= vocab: the columns of a
- *              padded head behind vocab take no part).  Aligned to its elements; rows of any alignment run at the same
- *              rate.  vocab is the call's own (1..2^22), not the model's.
+ *              padded head behind vocab take no part).  Aligned to its elements; rows of any alignment run at about the
+ *              same rate.  vocab is the call's own (1..2^22), not the model's.
  *   token_ids  device int32 [n], needed by logp; an id outside [0, vocab) is padding
  *   top_k      0..32
  * Outputs, device, each nullable (at least one, and top_ids where top_k > 0); with m = max_j x_j, L = log sum_j exp(x_j - m):
@@ -340,7 +340,7 @@ int mace_embed_tokens_grad(mace_handle_t h, const int32_t *token_ids, int32_t n,
  * A logit of -inf bans its token: probability 0, never listed.  The lowest finite value is an ordinary logit.  A row with nothing but
  * banned tokens: logp -inf, entropy 0, row_stats (-inf, 0).  A NaN or +inf among the vocab columns of a row: its outputs are
  * NaN (logp of padding 0) and its ids -1.  Statistics are fp32 whatever the logits' type, added in an order that depends on the sizes
- * alone.  workspace: mace_token_logprobs_workspace_bytes(h, n, vocab, top_k) bytes, 256-byte aligned, nothing of it read before it
+ * and on the rows' alignment alone.  workspace: mace_token_logprobs_workspace_bytes(h, n, vocab, top_k) bytes, 256-byte aligned, nothing of it read before it
  * is written.  Outputs and workspace overlap neither an input nor each other. */
 size_t mace_token_logprobs_workspace_bytes(mace_handle_t h, int32_t n, int32_t vocab, int32_t top_k);
 int mace_token_logprobs(mace_handle_t h, const void *logits, int32_t dtype, int32_t n, int32_t vocab, int64_t ld,

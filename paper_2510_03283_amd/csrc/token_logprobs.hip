@@ -18,8 +18,9 @@ constexpr float FAR = -1e4f, FAR2 = -1.4e4f;
 // Up to this magnitude of a row's maximum the rounding of its product with log2 e is a small part of an exponent (at most 0.06).
 constexpr float BIG = 1e6f;
 
-// 16 bytes of a row: 4 fp32 or 8 bf16 values.  Rows start at any element (odd vocabularies, padded heads), and a 16-byte access needs
-// no more than its elements' alignment: a wave's 1 KB then touches one cache line more.
+// 16 bytes of a row: 4 fp32 or 8 bf16 values.  Rows start at any element (odd vocabularies, padded heads).  A 16-byte access needs no more than
+// its elements' alignment, but a wave's 1 KB then touches one cache line more and, at an odd bf16 element, takes longer; long rows (LEAD) are cut where
+// their address is a multiple of a line's 128 bytes: their columns are counted from up to 63 places before the row, which are not read.
 typedef uint32_t u32x4_a4 __attribute__((ext_vector_type(4), aligned(4)));
 typedef uint32_t u32x4_a2 __attribute__((ext_vector_type(4), aligned(2)));
 typedef uint32_t u32x2_a2 __attribute__((ext_vector_type(2), aligned(2)));
@@ -39,22 +40,29 @@ struct Chunk {
     if constexpr (BF16) return __uint_as_float(i & 1 ? raw[i >> 1] & 0xffff0000u : raw[i >> 1] << 16);
     else return __uint_as_float(raw[i]);
   }
-  // columns col .. col + N - 1, -inf from `end` on
+  // columns col .. col + N - 1, -inf before 0 (LEAD) and from `end` on
+  template <bool LEAD>
   __device__ __forceinline__ void load_edge(const void *row, int col, int end) {
-    if (col + N <= end) return load<false>(row, col);
+    if ((!LEAD || col >= 0) && col + N <= end) return load<false>(row, col);
+    const auto there = [&](int c) { return LEAD ? (unsigned)c < (unsigned)end : c < end; };
     uint32_t w[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       if constexpr (BF16) {
-        const uint32_t lo = col + 2 * i < end ? ((const bf16_t *)row)[col + 2 * i] : 0xff80u, hi = col + 2 * i + 1 < end ? ((const bf16_t *)row)[col + 2 * i + 1] : 0xff80u;
+        const int c = col + 2 * i;
+        const uint32_t lo = there(c) ? ((const bf16_t *)row)[c] : 0xff80u, hi = there(c + 1) ? ((const bf16_t *)row)[c + 1] : 0xff80u;
         w[i] = lo | hi << 16;
       } else {
-        w[i] = col + i < end ? ((const uint32_t *)row)[col + i] : 0xff800000u;
+        w[i] = there(col + i) ? ((const uint32_t *)row)[col + i] : 0xff800000u;
       }
     }
     raw = raw_t{w[0], w[1], w[2], w[3]};
   }
 };
+
+constexpr int LINE = 128;
+template <bool BF16>
+__device__ __forceinline__ int lead_of(const void *row) { return (int)((uintptr_t)row % LINE) / (BF16 ? 2 : 4); }
 
 // The reference of a thread's terms: its maximum in units of log 2, ROUNDED - as a product that is never contracted into what uses it.
 __device__ __forceinline__ float reference_of(float m) {
@@ -197,7 +205,7 @@ __device__ __forceinline__ float kth_of_64(const float *set, int k) {
 
 // Leaves the columns whose value passes (strict ? > : >=) tau in S.c and returns their number, of which S.c holds CAND: lists the
 // groups whose maximum passes, and reads those again, eight loads of a wave at a time.
-template <bool BF16, int NT>
+template <bool BF16, int NT, bool LEAD>
 __device__ __forceinline__ int collect(TopScratch<NT> &S, const void *row, int c0, int c1, int n_groups, float tau, bool strict) {
   using T = Turn<BF16, NT>;
   constexpr int WAVES = T::WAVES, CAND = T::CAND;
@@ -220,7 +228,7 @@ __device__ __forceinline__ int collect(TopScratch<NT> &S, const void *row, int c
       const int g = __builtin_amdgcn_readfirstlane((int)S.list[i0 + k * WAVES]);
       first[k] = c0 + T::column(g / T::GROUPS, 0, 4 * (g % T::GROUPS));
 #pragma unroll
-      for (int e = 0; e < PER; ++e) x[k][e] = ld_io<BF16>(row, first[k] + min(in_group + e, c1 - 1 - first[k]));
+      for (int e = 0; e < PER; ++e) x[k][e] = ld_io<BF16>(row, LEAD ? max(0, min(first[k] + in_group + e, c1 - 1)) : first[k] + min(in_group + e, c1 - 1 - first[k]));
     }
     unsigned long long pass[AT_ONCE][PER];
     int total = 0, at = 0;
@@ -229,7 +237,7 @@ __device__ __forceinline__ int collect(TopScratch<NT> &S, const void *row, int c
       if (i0 + k * WAVES >= n) break;
 #pragma unroll
       for (int e = 0; e < PER; ++e) {
-        pass[k][e] = __ballot(in_group + e < c1 - first[k] && (strict ? x[k][e] > tau : x[k][e] >= tau));
+        pass[k][e] = __ballot((!LEAD || first[k] + in_group + e >= 0) && in_group + e < c1 - first[k] && (strict ? x[k][e] > tau : x[k][e] >= tau));
         total += __popcll(pass[k][e]);
       }
     }
@@ -263,7 +271,7 @@ __device__ __forceinline__ int rank_of(const Candidate *list, Candidate c, int n
 // More than CAND columns reach tau (many equal logits: a mask of the lowest value; a row in ascending order): tau is raised to the
 // k-th largest of NT columns above it until those above it fit, and if they are fewer than k, columns equal to tau fill up,
 // from the lowest on.
-template <bool BF16, int NT>
+template <bool BF16, int NT, bool LEAD>
 __device__ __noinline__ int best_columns_crowded(TopScratch<NT> &S, const void *row, int c0, int c1, int n_groups, int k, float tau) {
   constexpr int WAVES = NT / 64, CAND = Turn<BF16, NT>::CAND;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -272,7 +280,7 @@ __device__ __noinline__ int best_columns_crowded(TopScratch<NT> &S, const void *
     __syncthreads();
     if (threadIdx.x == 0) S.n_list = S.n_cand = 0;
     __syncthreads();
-    n = collect<BF16, NT>(S, row, c0, c1, n_groups, tau, true);
+    n = collect<BF16, NT, LEAD>(S, row, c0, c1, n_groups, tau, true);
     if (n <= CAND) break;
     const Candidate c = S.c[threadIdx.x];
     if (rank_of(S.c, c, NT) == k - 1) S.tau = value_of(c);
@@ -282,7 +290,7 @@ __device__ __noinline__ int best_columns_crowded(TopScratch<NT> &S, const void *
   const int above = n;
   for (int c = c0; c < c1 && n < k; c += NT) {
     const int col = c + threadIdx.x;
-    const bool tie = col < c1 && ld_io<BF16>(row, col) == tau;
+    const bool tie = (unsigned)col < (unsigned)c1 && ld_io<BF16>(row, col) == tau;
     const unsigned long long b = __ballot(tie);
     __syncthreads();
     if (lane == 0) S.scan[wave] = __popcll(b);
@@ -304,7 +312,7 @@ __device__ __noinline__ int best_columns_crowded(TopScratch<NT> &S, const void *
 // -64 log(1 - k / 64) where the values are spread by chance: 24 for k = 20, 44 for k = 32.  The groups whose maximum reaches tau, about as
 // many, are read again, 256 bytes each.
 // meanwhile: what the last wave does while the first looks for tau.
-template <bool BF16, int NT, typename F>
+template <bool BF16, int NT, bool LEAD, typename F>
 __device__ __forceinline__ int best_columns(TopScratch<NT> &S, const void *row, int c0, int c1, int turns, int k, float m, F meanwhile) {
   using T = Turn<BF16, NT>;
   constexpr int SET = NT / 64;                   // threads of a set
@@ -321,8 +329,8 @@ __device__ __forceinline__ int best_columns(TopScratch<NT> &S, const void *row, 
   if (threadIdx.x >= NT - 64) meanwhile();
   __syncthreads();
   const float tau = S.tau;
-  const int n = collect<BF16, NT>(S, row, c0, c1, n_groups, tau, false);
-  return n <= T::CAND ? n : best_columns_crowded<BF16, NT>(S, row, c0, c1, n_groups, k, tau);
+  const int n = collect<BF16, NT, LEAD>(S, row, c0, c1, n_groups, tau, false);
+  return n <= T::CAND ? n : best_columns_crowded<BF16, NT, LEAD>(S, row, c0, c1, n_groups, k, tau);
 }
 
 // Floats of the partial results of one part when a row is shared by several blocks: State, then the part's alternatives, best first.
@@ -333,7 +341,7 @@ __host__ __device__ __forceinline__ size_t part_floats(int k) { return (size_t)(
 // delta = m log2 e - m2, which is taken out at the end (it is the term of the maximum itself).
 // 32768 x 32000 fp32: 600 us, 7.0 TB/s, HBM-bound.  2048 x 128011 bf16 with 8 alternatives: 91 us, 5.8 TB/s, bound by vector instructions (a logit takes about 9
 // slots, four of them its exponential).  One row of 32000 with 5 alternatives: 7 us, a chain of four turns, three reductions and a second look at some groups.
-template <bool BF16, bool ENT, bool TOP, int NT, bool STREAM>
+template <bool BF16, bool ENT, bool TOP, int NT, bool STREAM, bool LEAD>
 __global__ __launch_bounds__(NT, NT == 64 ? 5 : 1) void token_logprobs_kernel(const TokenLogprobs a, int parts, int part_turns, float *__restrict__ scratch) {
   using T = Turn<BF16, NT>;
   constexpr int WAVES = T::WAVES;
@@ -344,18 +352,18 @@ __global__ __launch_bounds__(NT, NT == 64 ? 5 : 1) void token_logprobs_kernel(co
     const long long r = parts == 1 ? w : w / parts;
     const int part = (int)(w - r * parts);
     const void *row = (const char *)a.logits + (size_t)r * a.ld * (BF16 ? 2 : 4);
-    const int c0 = part * part_turns * T::COLS, c1 = min((long long)a.vocab, (long long)c0 + part_turns * T::COLS);
+    const int c0 = part * part_turns * T::COLS - (LEAD ? lead_of<BF16>(row) : 0), c1 = min(a.vocab, c0 + part_turns * T::COLS);
     const int turns = (c1 - c0 + T::COLS - 1) / T::COLS;
     const int tok = parts == 1 && a.logp ? a.token_ids[r] : -1;          // asked for ahead of the row, used behind it
     float m = -INFINITY, m2 = -BIG * LOG2E, s = 0.f, u = 0.f;
     Chunk<BF16> next[U];
     const auto ask = [&](int t) {
-      if (c0 + (t + 1) * T::COLS <= c1) {
+      if ((!LEAD || c0 + t * T::COLS >= 0) && c0 + (t + 1) * T::COLS <= c1) {
 #pragma unroll
         for (int i = 0; i < U; ++i) next[i].template load<STREAM>(row, c0 + T::column(t, i, threadIdx.x));
       } else {
 #pragma unroll
-        for (int i = 0; i < U; ++i) next[i].load_edge(row, c0 + T::column(t, i, threadIdx.x), c1);
+        for (int i = 0; i < U; ++i) next[i].template load_edge<LEAD>(row, c0 + T::column(t, i, threadIdx.x), c1);
       }
     };
     ask(0);
@@ -446,7 +454,7 @@ __global__ __launch_bounds__(NT, NT == 64 ? 5 : 1) void token_logprobs_kernel(co
       if (threadIdx.x >= NT - 64) results();
     } else {
       const int k = a.top_k;
-      const int n = best_columns<BF16, NT>(S, row, c0, c1, turns, k, m, [&]() {
+      const int n = best_columns<BF16, NT, LEAD>(S, row, c0, c1, turns, k, m, [&]() {
         results();
         if (writer) S.row = o;
       });
@@ -538,23 +546,23 @@ __device__ __forceinline__ void put(char *out, size_t at, V v) {
   else *(V *)(out + at) = v;
 }
 // A wave takes 64 x U 16-byte accesses of a row; HBM-bound, one read and one write a logit (16384 x 32000 fp32 to bf16: 522 us, 6.0 TB/s).
-template <bool BF16, bool OUT_BF16, bool STREAM>
+template <bool BF16, bool OUT_BF16, bool LEAD, bool STREAM>
 __global__ __launch_bounds__(256) void token_logprobs_grad_kernel(const TokenLogprobsGrad a, int parts) {
   constexpr int N = Chunk<BF16>::N;
   const int lane = threadIdx.x & 63;
   for (long long w = (long long)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); w < (long long)a.n * parts; w += (long long)gridDim.x * 4) {
     const long long r = parts == 1 ? w : w / parts;
-    const int c0 = (int)(w - r * parts) * 64 * U * N;
+    const void *row = (const char *)a.logits + (size_t)r * a.ld * (BF16 ? 2 : 4);
+    char *out = (char *)a.d_logits + (size_t)r * a.ld_d * (OUT_BF16 ? 2 : 4);
+    const int c0 = (int)(w - r * parts) * 64 * U * N - (LEAD ? lead_of<OUT_BF16>(out) : 0);
     const int tok = a.d_logp ? a.token_ids[r] : -1;
     const float g = tok >= 0 && tok < a.vocab ? a.d_logp[r] : 0.f, h = a.d_entropy ? a.d_entropy[r] : 0.f;
     const float m = a.row_stats[2 * r], L = a.row_stats[2 * r + 1], H = a.d_entropy ? a.entropy[r] : 0.f;
     const bool zero = m == -INFINITY || (g == 0.f && h == 0.f);
-    const void *row = (const char *)a.logits + (size_t)r * a.ld * (BF16 ? 2 : 4);
-    char *out = (char *)a.d_logits + (size_t)r * a.ld_d * (OUT_BF16 ? 2 : 4);
     Chunk<BF16> x[U];
     if (!zero) {
 #pragma unroll
-      for (int i = 0; i < U; ++i) x[i].load_edge(row, c0 + (i * 64 + lane) * N, a.vocab);
+      for (int i = 0; i < U; ++i) x[i].template load_edge<LEAD>(row, c0 + (i * 64 + lane) * N, a.vocab);
     }
 #pragma unroll
     for (int i = 0; i < U; ++i) {
@@ -566,7 +574,7 @@ __global__ __launch_bounds__(256) void token_logprobs_grad_kernel(const TokenLog
         const float lp = x[i].get(j) - m - L, p = exp_of(lp);
         o[j] = (col + j == tok ? g : 0.f) - g * p - h * p * (fmaxf(lp, FAR) + H);
       }
-      if (col + N <= a.vocab) {
+      if ((!LEAD || col >= 0) && col + N <= a.vocab) {
         if constexpr (OUT_BF16) {
           if constexpr (BF16) put<u32x4_a2, STREAM>(out, (size_t)col * 2, u32x4_a2{cvt_pk_bf16(o[0], o[1]), cvt_pk_bf16(o[2], o[3]), cvt_pk_bf16(o[4], o[5]), cvt_pk_bf16(o[6], o[7])});
           else put<u32x2_a2, STREAM>(out, (size_t)col * 2, u32x2_a2{cvt_pk_bf16(o[0], o[1]), cvt_pk_bf16(o[2], o[3])});
@@ -577,37 +585,49 @@ __global__ __launch_bounds__(256) void token_logprobs_grad_kernel(const TokenLog
       } else {
 #pragma unroll
         for (int j = 0; j < N; ++j)
-          if (col + j < a.vocab) st_io<OUT_BF16>(out, col + j, o[j]);
+          if ((!LEAD || col + j >= 0) && col + j < a.vocab) st_io<OUT_BF16>(out, col + j, o[j]);
       }
     }
   }
 }
+
+// Places that a row can lie behind the beginning of a line; whether any row does.
+constexpr int most_lead(bool bf16) { return LINE / (bf16 ? 2 : 4) - 1; }
+bool off_lines(const void *rows, long long ld, bool bf16) { return ((uintptr_t)rows | (uintptr_t)(ld * (bf16 ? 2 : 4))) % LINE != 0; }
 
 // Blocks (parts) of a row: where there are fewer than 512 rows, parts of eight turns (32768 fp32 columns), below which joining them costs more
 // than they save.  us with 20 alternatives, one part / parts of eight turns / of four: one row of 32000 fp32 logits 8.9 / 8.9 / 11.9, one
 // of 128011 20.2 / 12.8 / 11.8, 64 of 32000 9.9 / 9.9 / 13.7, 64 of 128011 28.0 / 16.5 / 18.0, 256 of 128011 41.4 / 33.9 / 37.  Counted for fp32 whatever the type, so that the scratch does not depend on it.
 int parts_of(int n, int vocab) {
   using T = Turn<false, 256>;
-  const int turns = (vocab + T::COLS - 1) / T::COLS, least = (turns + T::MAX_TURNS - 1) / T::MAX_TURNS;
+  const int turns = (vocab + most_lead(false) + T::COLS - 1) / T::COLS, least = (turns + T::MAX_TURNS - 1) / T::MAX_TURNS;
   return std::max(least, std::min({512 / n, turns / 8, 64}));
 }
 
-template <bool BF16, bool ENT, int NT>
-auto rows_kernel(bool top, bool stream) {
-  return top ? (stream ? token_logprobs_kernel<BF16, ENT, true, NT, true> : token_logprobs_kernel<BF16, ENT, true, NT, false>)
-             : (stream ? token_logprobs_kernel<BF16, ENT, false, NT, true> : token_logprobs_kernel<BF16, ENT, false, NT, false>);
+template <bool BF16, bool ENT, bool TOP, int NT>
+auto rows_kernel(bool stream, bool lead) {
+  if constexpr (NT == 256)
+    if (lead && stream) return token_logprobs_kernel<BF16, ENT, TOP, NT, true, true>;
+  if constexpr (NT == 256 && BF16)
+    if (lead) return token_logprobs_kernel<BF16, ENT, TOP, NT, false, true>;
+  return stream ? token_logprobs_kernel<BF16, ENT, TOP, NT, true, false> : token_logprobs_kernel<BF16, ENT, TOP, NT, false, false>;
 }
 template <bool BF16, int NT>
 hipError_t launch_rows(const TokenLogprobs &a, int parts, float *scratch, hipStream_t st) {
   using T = Turn<BF16, NT>;
-  const int turns = (a.vocab + T::COLS - 1) / T::COLS, part_turns = (turns + parts - 1) / parts;
-  parts = (turns + part_turns - 1) / part_turns;
   // Logits that the last-level cache (256 MB) cannot hold are read past it: 16384 x 32000 fp32 354 -> 317 us, 2048 x 32000 49.0 -> 42.5; of
   // fewer the cache may hold what their producer left (512 x 32000, resident: 12.6 -> 13.3).
   const bool stream = (size_t)a.n * a.vocab * (BF16 ? 2 : 4) > LLC_BYTES;
+  // Where rows do not begin with a line, us without / with a lead: 2048 x 128011 fp32 170 / 156, 2048 x 50257 69 / 65, but 512 x 31999 12.6 / 12.8, 4096 x 31999
+  // with 8 alternatives 92 / 98; bf16, every other row at an odd element, 2048 x 128011 119 / 96, 4096 x 31999 63 / 58, 1024 x 31999 17.1 / 16.3, 4096 x 15999 40.3 / 36.3, but
+  // 512 x 31999 9.8 / 10.3, 1024 x 8191 7.4 / 11.0.
+  const bool lead = NT == 256 && off_lines(a.logits, a.ld, BF16) && (BF16 ? a.vocab >= 12288 && (long long)a.n * a.vocab >= 30 << 20 : stream && a.vocab >= 49152);
+  const int turns = (a.vocab + (lead ? most_lead(BF16) : 0) + T::COLS - 1) / T::COLS, part_turns = (turns + parts - 1) / parts;
+  parts = (turns + part_turns - 1) / part_turns;
   const dim3 grid((unsigned)std::min<long long>((long long)a.n * parts, 1 << 22));
   // Without the entropy its sum is left out as well: 2048 x 128011 bf16 115 -> 110 us, one row of 32000 4.9 -> 4.3, 16384 x 32000 186 -> 173.
-  auto *k = a.entropy ? rows_kernel<BF16, true, NT>(a.top_k > 0, stream) : rows_kernel<BF16, false, NT>(a.top_k > 0, stream);
+  auto *k = a.entropy ? (a.top_k ? rows_kernel<BF16, true, true, NT>(stream, lead) : rows_kernel<BF16, true, false, NT>(stream, lead))
+                      : (a.top_k ? rows_kernel<BF16, false, true, NT>(stream, lead) : rows_kernel<BF16, false, false, NT>(stream, lead));
   hipLaunchKernelGGL(k, grid, dim3(NT), 0, st, a, parts, part_turns, scratch);
   if (parts > 1) hipLaunchKernelGGL(token_logprobs_join_kernel<BF16>, dim3((unsigned)std::min(a.n, 1 << 22)), dim3(JOIN_NT), 0, st, a, parts, (const float *)scratch);
   return hipGetLastError();
@@ -628,6 +648,12 @@ hipError_t launch_rows(const TokenLogprobs &a, float *scratch, hipStream_t st) {
   return wide ? launch_rows<BF16, 512>(a, parts, scratch, st) : launch_rows<BF16, 256>(a, parts, scratch, st);
 }
 
+template <bool BF16, bool OUT_BF16>
+auto grad_kernel(bool lead, bool stream) {
+  return lead ? (stream ? token_logprobs_grad_kernel<BF16, OUT_BF16, true, true> : token_logprobs_grad_kernel<BF16, OUT_BF16, true, false>)
+              : (stream ? token_logprobs_grad_kernel<BF16, OUT_BF16, false, true> : token_logprobs_grad_kernel<BF16, OUT_BF16, false, false>);
+}
+
 }  // namespace
 
 size_t token_logprobs_scratch_bytes(int n, int vocab, int top_k) {
@@ -643,13 +669,14 @@ hipError_t launch_token_logprobs(const TokenLogprobs &a, bool bf16, void *scratc
 
 hipError_t launch_token_logprobs_grad(const TokenLogprobsGrad &a, bool bf16, bool out_bf16, hipStream_t st) {
   if (a.n <= 0) return hipSuccess;
-  const int cols = 64 * U * (bf16 ? 8 : 4), parts = (a.vocab + cols - 1) / cols;
+  // Whole lines written where rows do not begin with one, us without / with a lead: 8192 x 31999 fp32 427 / 408, bf16 232 / 196, 2048 x 128011 bf16 204 / 184, 16000 x 8191
+  // 111 / 101, but 30000 x 4097 99 / 110.
+  const bool lead = a.vocab >= 8192 && off_lines(a.d_logits, a.ld_d, out_bf16);
+  const int cols = 64 * U * (bf16 ? 8 : 4), parts = (a.vocab + (lead ? most_lead(out_bf16) : 0) + cols - 1) / cols;
   // Gradients that the last-level cache cannot hold are written past it: 16384 x 32000 bf16 555 -> 536 us.
   const bool stream = (size_t)a.n * a.vocab * (out_bf16 ? 2 : 4) > LLC_BYTES;
-  auto *k = bf16 ? (out_bf16 ? (stream ? token_logprobs_grad_kernel<true, true, true> : token_logprobs_grad_kernel<true, true, false>)
-                             : (stream ? token_logprobs_grad_kernel<true, false, true> : token_logprobs_grad_kernel<true, false, false>))
-                 : (out_bf16 ? (stream ? token_logprobs_grad_kernel<false, true, true> : token_logprobs_grad_kernel<false, true, false>)
-                             : (stream ? token_logprobs_grad_kernel<false, false, true> : token_logprobs_grad_kernel<false, false, false>));
+  auto *k = bf16 ? (out_bf16 ? grad_kernel<true, true>(lead, stream) : grad_kernel<true, false>(lead, stream))
+                 : (out_bf16 ? grad_kernel<false, true>(lead, stream) : grad_kernel<false, false>(lead, stream));
   hipLaunchKernelGGL(k, dim3((unsigned)std::min<long long>(((long long)a.n * parts + 3) / 4, 1 << 22)), dim3(256), 0, st, a, parts);
   return hipGetLastError();
 }

@@ -124,7 +124,7 @@ def draw(torch, n, vocab, kind, seed):
     return x, token
 
 
-SHAPES = [(1, 1), (2, 3), (5, 64), (9, 255), (3, 1000), (17, 2048), (300, 777), (1, 32000), (40, 32000), (600, 4099), (2, 128011), (33, 50001)]
+SHAPES = [(1, 1), (2, 3), (5, 64), (9, 255), (3, 1000), (17, 2048), (300, 777), (1, 32000), (40, 32000), (600, 4099), (2, 128011), (33, 50001), (1000, 33001), (1400, 50001)]
 
 
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
@@ -142,7 +142,7 @@ def test_sizes(torch_mod, lib, dtype, n, vocab):
 
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
 @pytest.mark.parametrize("kind", ["plain", "peaked", "banned", "lowest", "equal", "coarse", "rising", "falling", "large"])
-@pytest.mark.parametrize("n,vocab,k", [(12, 70, 32), (37, 2048, 20), (21, 31999, 32), (7, 131072, 8), (1100, 1003, 4), (300, 12301, 20), (9, 6145, 24)])
+@pytest.mark.parametrize("n,vocab,k", [(12, 70, 32), (37, 2048, 20), (21, 31999, 32), (7, 131072, 8), (1100, 1003, 4), (300, 12301, 20), (9, 6145, 24), (1000, 33001, 20)])
 def test_values(torch_mod, lib, dtype, kind, n, vocab, k):
     torch = torch_mod
     x, token = draw(torch, n, vocab, kind, 11 + n)
@@ -318,7 +318,7 @@ def grad_check(torch, lib, x, token, dtype, out, entropy, logp, ld_out=None, in_
 
 @pytest.mark.parametrize("dtype,out", [("fp32", "fp32"), ("fp32", "bf16"), ("bf16", "bf16"), ("bf16", "fp32")])
 @pytest.mark.parametrize("n,vocab,ld,offset,ld_out", [(1, 1, 1, 0, 1), (7, 3, 5, 1, 4), (33, 255, 256, 0, 256), (12, 2048, 2048, 0, 2048), (21, 4097, 4099, 3, 4097),
-                                                       (5, 32000, 32000, 0, 32064), (3, 128011, 128064, 0, 128011), (1500, 100, 100, 2, 100)])
+                                                       (5, 32000, 32000, 0, 32064), (3, 128011, 128064, 0, 128011), (1500, 100, 100, 2, 100), (30, 9001, 9003, 1, 9005)])
 def test_gradient(torch_mod, lib, dtype, out, n, vocab, ld, offset, ld_out):
     torch = torch_mod
     x, token = draw(torch, n, vocab, "banned" if n > 20 else "peaked", n)
@@ -330,7 +330,7 @@ def test_gradient(torch_mod, lib, dtype, out, n, vocab, ld, offset, ld_out):
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
 def test_gradient_in_place(torch_mod, lib, dtype):
     torch = torch_mod
-    for vocab, ld, offset in ((2048, 2048, 0), (1001, 1003, 1)):
+    for vocab, ld, offset in ((2048, 2048, 0), (1001, 1003, 1), (9001, 9003, 5)):
         x, token = draw(torch, 50, vocab, "banned", 6)
         rows = rows_of(torch, x, ld, offset, dtype)
         grad_check(torch, lib, rows, token, dtype, dtype, True, True, in_place=True)
