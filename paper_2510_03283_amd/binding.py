@@ -186,9 +186,7 @@ def _host_i32(t):
 
 def _stream(stream=None):
     """hipStream_t of a torch stream; without one, of the current stream (asked for by its number: 0.1 us a call, the object takes 2.7)."""
-    if stream is not None:
-        return C.c_void_p(stream.cuda_stream)
-    return C.c_void_p(torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()))
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()) if stream is None else stream.cuda_stream
 
 
 class Handle(C.c_void_p):
@@ -376,7 +374,7 @@ def _tensor(h, t, name: str, dtype, shape):
     """Pointer of an optional tensor on the handle's device, contiguous and of this type and shape (the library is told sizes only)."""
     if t is None:
         return None
-    if t.get_device() != h.device or t.dtype != dtype or t.shape != shape or not t.is_contiguous():
+    if t.dtype != dtype or t.shape != shape or t.get_device() != h.device or not t.is_contiguous():
         raise MaceError(f"{name}: a contiguous tensor of {dtype} {tuple(shape)} on cuda:{h.device} is wanted, got {t.dtype} {tuple(t.shape)} on {t.device}")
     return t.data_ptr()
 
@@ -396,7 +394,9 @@ def _rows(h, t, name: str, vocab):
 
 
 def _workspace(h, t):
-    return _tensor(h, t, "workspace", t.dtype, t.shape), t.numel() * t.element_size()
+    if t.get_device() != h.device or not t.is_contiguous():
+        raise MaceError(f"workspace: a contiguous tensor on cuda:{h.device} is wanted, got one on {t.device}")
+    return t.data_ptr(), t.nbytes
 
 
 def mace_embed_tokens(h, table, token_ids, out, scale: float = 1.0, stream=None):
