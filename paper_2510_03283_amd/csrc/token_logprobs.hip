@@ -341,7 +341,7 @@ __host__ __device__ __forceinline__ size_t part_floats(int k) { return (size_t)(
 // delta = m log2 e - m2, which is taken out at the end (it is the term of the maximum itself).
 // 32768 x 32000 fp32: 600 us, 7.0 TB/s, HBM-bound.  2048 x 128011 bf16 with 8 alternatives: 91 us, 5.8 TB/s, bound by vector instructions (a logit takes about 9
 // slots, four of them its exponential).  One row of 32000 with 5 alternatives: 7 us, a chain of four turns, three reductions and a second look at some groups.
-// Waves a SIMD, where the compiler's own choice of registers is not best: us with 4 / 5 / 6, 16384 x 32000 bf16 with 8 alternatives 230 / 214 / 231, 2048 x 128064 96 / 93.5 / 102, but
+// Waves a SIMD, where the compiler's own choice of registers is not best: us with 4 / 5 / 6, 16384 x 32000 bf16 with 8 alternatives 236 / 220 / 231, 2048 x 128064 96 / 96 / 102, but
 // 16384 x 32000 fp32 331 / 355 / 349; 64 threads, 30000 x 2048 bf16 5 / 6 67.6 / 75.6.
 constexpr int waves_wanted(bool bf16, bool top, int nt) { return nt == 64 || (nt == 256 && bf16 && top) ? 5 : 1; }
 template <bool BF16, bool ENT, bool TOP, int NT, bool STREAM, bool LEAD>
