@@ -613,7 +613,8 @@ auto rows_kernel(bool stream, bool lead) {
     if (lead && stream) return token_logprobs_kernel<BF16, ENT, TOP, NT, true, true>;
   if constexpr (NT == 256 && BF16)
     if (lead) return token_logprobs_kernel<BF16, ENT, TOP, NT, false, true>;
-  return stream ? token_logprobs_kernel<BF16, ENT, TOP, NT, true, false> : token_logprobs_kernel<BF16, ENT, TOP, NT, false, false>;
+  if constexpr (NT == 512) return token_logprobs_kernel<BF16, ENT, TOP, NT, false, false>;      // (256 parts of 131072 columns at most: never past the cache)
+  else return stream ? token_logprobs_kernel<BF16, ENT, TOP, NT, true, false> : token_logprobs_kernel<BF16, ENT, TOP, NT, false, false>;
 }
 template <bool BF16, int NT>
 hipError_t launch_rows(const TokenLogprobs &a, int parts, float *scratch, hipStream_t st) {

@@ -96,3 +96,26 @@ def test_workspace_of_more_rows_serves_fewer(recorder):
     assert need == sorted(need)
     for vocab, k in ((100, 0), (2048, 5), (32000, 0), (32000, 20), (128011, 32), (1 << 22, 1)):
         assert all(recorder("logprobs", n=n, vocab=vocab, top_k=k)[3] >= 256 for n in (1, 7, 300, 5000))
+
+
+def built_kernels(source):
+    """Names of the kernels that were built from a source (their handles in its object)."""
+    from paper_2510_03283_amd import build
+    lines = subprocess.run(["nm", os.path.join(build.BUILD_DIR, source + ".o")], capture_output=True, text=True, check=True).stdout.splitlines()
+    return {l.split()[-1] for l in lines if "_kernel" in l and "__device_stub__" not in l}
+
+
+def launched(recorder, call, every):
+    return {l["kernel"] for opts in every for l in recorder(call, **opts)[2]}
+
+
+def test_every_log_probability_kernel_is_reached(recorder):
+    """A variant that no call can take is dead code that no test can run either."""
+    rows = [dict(n=5000, vocab=1000), dict(n=8400, vocab=8192), dict(n=17000, vocab=8192),                    # a wave a row; past the cache
+            dict(n=1, vocab=32000), dict(n=128, vocab=131072), dict(n=1, vocab=1 << 22),                          # 512 threads; shared rows
+            dict(n=1000, vocab=32000), dict(n=1000, vocab=32001),                                               # 256 threads; off the lines
+            dict(n=6000, vocab=50304), dict(n=6000, vocab=50257)]
+    got = launched(recorder, "logprobs", [{**r, "dtype": t, "top_k": k, **e} for r in rows for t in (0, 1) for k in (0, 5) for e in ({}, dict(null="entropy"))])
+    grads = [dict(n=100, vocab=1000), dict(n=100, vocab=9001), dict(n=5000, vocab=32000), dict(n=5000, vocab=32001)]
+    got |= launched(recorder, "logprobs_grad", [{**r, "dtype": t, "d_dtype": o} for r in grads for t in (0, 1) for o in (0, 1)])
+    assert got == built_kernels("token_logprobs")
