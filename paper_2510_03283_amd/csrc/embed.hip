@@ -48,7 +48,7 @@ __global__ __launch_bounds__(256) void embed_rows_kernel(const void *__restrict_
 }
 
 // ------------------------------------------------------------------ gradient of the table
-// Two to four launches (one for few rows), no block of which waits for another, and no order of which depends on which block comes first.
+// Three or four launches (one for few rows), no block of which waits for another, and no order of which depends on which block comes first.
 //  bucket (many rows only) The ids are cut into chunks of 1024 rows; a block sorts its chunk by bucket, 2^lg adjacent tokens (stable: rows of a bucket
 //         keep their order), and notes how many rows each bucket has in it.
 //  place  A block per bucket collects the bucket's rows from all chunks in order and sorts them by token, again stably.  The rows of
@@ -480,11 +480,9 @@ hipError_t launch_embed_grad(const int32_t *ids, int n, int vocab, int d, const 
               : past     ? (stream ? embed_sum_kernel<false, true, true> : embed_sum_kernel<false, false, true>)
                          : (stream ? embed_sum_kernel<false, true, false> : embed_sum_kernel<false, false, false>);
   hipLaunchKernelGGL(sum, blocks(p.windows * p.strips + zero_units), dim3(256), 0, st, starts, order, dx, vocab, d, scale, d_table, aside, p.window, p.windows, p.strips);
-  if (p.windows > 1) {
-    const int strips = (d + 1023) / 1024;
-    const dim3 joins((unsigned)std::min<long long>(p.windows * strips, 1 << 22));
-    auto *join = accumulate ? embed_join_kernel<true> : embed_join_kernel<false>;
-    hipLaunchKernelGGL(join, joins, dim3(256), 0, st, starts, order, vocab, d, scale, d_table, aside, p.window, p.windows, strips);
-  }
+  const int join_strips = (d + 1023) / 1024;
+  const dim3 joins((unsigned)std::min<long long>(p.windows * join_strips, 1 << 22));       // (more than FEW_ROWS rows: always several windows)
+  auto *join = accumulate ? embed_join_kernel<true> : embed_join_kernel<false>;
+  hipLaunchKernelGGL(join, joins, dim3(256), 0, st, starts, order, vocab, d, scale, d_table, aside, p.window, p.windows, join_strips);
   return hipGetLastError();
 }

@@ -119,3 +119,18 @@ def test_every_log_probability_kernel_is_reached(recorder):
     grads = [dict(n=100, vocab=1000), dict(n=100, vocab=9001), dict(n=5000, vocab=32000), dict(n=5000, vocab=32001)]
     got |= launched(recorder, "logprobs_grad", [{**r, "dtype": t, "d_dtype": o} for r in grads for t in (0, 1) for o in (0, 1)])
     assert got == built_kernels("token_logprobs")
+
+
+def test_every_embedding_kernel_is_reached(recorder):
+    got = launched(recorder, "embed", [dict(n=n, bf16=b) for n in (100, 300000) for b in (0, 1)])
+    got |= launched(recorder, "embed_grad", [dict(n=n, V=V, accumulate=a) for n in (100, 1000, 5000, 300000) for V in (2048, 320000) for a in (0, 1)])
+    assert got == built_kernels("embed")
+
+
+def test_launches_of_the_table_gradient(recorder):
+    """One for up to 256 rows, else place, sum and join, with the bucket kernel before them from 8193 rows on."""
+    for n, names in ((0, ["few"]), (1, ["few"]), (256, ["few"]), (257, ["place", "sum", "join"]), (8192, ["place", "sum", "join"]), (8193, ["bucket", "place", "sum", "join"]),
+                     (70000, ["bucket", "place", "sum", "join"])):
+        for d in (64, 256, 8192):
+            kernels = [l["kernel"] for l in recorder("embed_grad", n=n, d=d)[2]]
+            assert len(kernels) == len(names) and all(f"embed_{a}_kernel" in k for a, k in zip(names, kernels)), (n, d)
