@@ -2,6 +2,7 @@
 launched) and what they launch (token_ops_recorder.cpp)."""
 import json
 import os
+import re
 import subprocess
 
 import pytest
@@ -134,3 +135,33 @@ def test_launches_of_the_table_gradient(recorder):
         for d in (64, 256, 8192):
             kernels = [l["kernel"] for l in recorder("embed_grad", n=n, d=d)[2]]
             assert len(kernels) == len(names) and all(f"embed_{a}_kernel" in k for a, k in zip(names, kernels)), (n, d)
+
+
+def kernel(recorder, call, name, **opts):
+    """Template arguments of the launched kernel of this name, in order."""
+    found = [l["kernel"] for l in recorder(call, **opts)[2] if name in l["kernel"]]
+    assert len(found) == 1, (call, opts, found)
+    return [int(a) for a in re.findall(r"L[bi](\d+)E", found[0].split(name)[1].split("EE")[0] + "E")]
+
+
+def test_large_cases_take_the_variants_that_they_are_for(recorder):
+    """The sizes of the GPU tests past the last-level cache, by the kernels that are launched for them."""
+    import test_gpu_token_variants as v
+    code = {"fp32": 0, "bf16": 1}
+    taken = set()
+    for n, vocab, ld, offset, dtype in v.WAVE_ROWS_PAST + v.ROWS_PAST:
+        for k in (0, 8):
+            bf16, entropy, top, threads, past, lead = kernel(recorder, "logprobs", "token_logprobs_kernel", n=n, vocab=vocab, ld=ld, dtype=code[dtype], top_k=k,
+                                                             misalign="logits", by=offset * v.size(dtype))
+            assert (bf16, entropy, top, past) == (code[dtype], 1, k > 0, 1)
+            taken.add((bf16, threads, lead))
+    assert taken == {(0, 64, 0), (1, 64, 0), (0, 256, 0), (0, 256, 1), (1, 256, 0), (1, 256, 1)}
+    for n, vocab in v.WAVE_ROWS:
+        assert all(kernel(recorder, "logprobs", "token_logprobs_kernel", n=n, vocab=vocab, dtype=t, top_k=20)[3:] == [64, 0, 0] for t in (0, 1))
+    for n, vocab, out, odd in v.GRADS_PAST:
+        for t in (0, 1):
+            assert kernel(recorder, "logprobs_grad", "token_logprobs_grad_kernel", n=n, vocab=vocab, ld=vocab + odd, ld_d=vocab + odd, dtype=t, d_dtype=code[out]) == [t, code[out], odd, 1]
+    for n, d, bf16 in v.EMBED_PAST:
+        assert kernel(recorder, "embed", "embed_rows_kernel", n=n, d=d, bf16=int(bf16)) == [int(bf16), 1]
+    assert [kernel(recorder, "embed_grad", "embed_sum_kernel", n=n, d=d, V=V, accumulate=a) for n, d, V in v.TABLE_PAST for a in (0, 1)] == [[0, 1, 0], [1, 1, 0], [0, 1, 1], [1, 1, 0]]
+    assert [kernel(recorder, "embed_grad", "embed_few_kernel", n=n, d=d, V=V, accumulate=0) for n, d, V in v.FEW_PAST] == [[0, 1]] * 2
