@@ -161,3 +161,23 @@ FEW_PAST = [(100, 4096, 32000), (0, 4096, 32000)]
 def test_table_gradient_past_the_cache(torch_mod, accumulate, n, d, vocab):
     assert 8 * n * d >= LLC or 4 * vocab * d > LLC
     embed.check_grad(torch_mod, d, vocab, embed.draw_ids(torch_mod, "text", n, vocab, n), accumulate, 0.7)
+
+
+# ---- what lies behind the workspace
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("n,vocab", [(1, 32000), (1, 65505), (1, 65536), (3, 128011), (2, 131072), (7, 262145), (64, 128011), (170, 98304), (255, 66000), (511, 140001), (600, 131073)])
+def test_nothing_is_written_behind_the_workspace(torch_mod, lib, dtype, n, vocab):  # noqa: F811
+    """Rows that several blocks share, around the sizes where their number changes."""
+    torch = torch_mod
+    x, token = logprobs.draw(torch, n, vocab, "plain", n)
+    for ld, offset, k in ((vocab + -vocab % 64, 0, 32), (vocab + 1, 1, 0), (vocab, 63, 1)):
+        rows = logprobs.rows_of(torch, x, ld, offset, dtype)
+        o = logprobs.call(torch, lib, rows, token, k)
+        torch.cuda.synchronize()
+        logprobs.check(torch, rows, token, o, k)
+
+
+@pytest.mark.parametrize("n,d,vocab", [(257, 64, 64), (300, 8192, 640), (1024, 256, 2048), (4096, 1024, 2048), (4097, 64, 2048), (8192, 64, 2048), (8193, 2048, 2048), (16385, 128, 300032)])
+def test_nothing_is_written_behind_the_gradients_workspace(torch_mod, n, d, vocab):
+    for kind in ("one", "text", "runs"):                                      # all sums, some and few set aside
+        embed.check_grad(torch_mod, d, vocab, embed.draw_ids(torch_mod, kind, n, vocab, n), kind == "text", 1.0)

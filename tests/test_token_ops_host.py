@@ -165,3 +165,34 @@ def test_large_cases_take_the_variants_that_they_are_for(recorder):
         assert kernel(recorder, "embed", "embed_rows_kernel", n=n, d=d, bf16=int(bf16)) == [int(bf16), 1]
     assert [kernel(recorder, "embed_grad", "embed_sum_kernel", n=n, d=d, V=V, accumulate=a) for n, d, V in v.TABLE_PAST for a in (0, 1)] == [[0, 1, 0], [1, 1, 0], [0, 1, 1], [1, 1, 0]]
     assert [kernel(recorder, "embed_grad", "embed_few_kernel", n=n, d=d, V=V, accumulate=0) for n, d, V in v.FEW_PAST] == [[0, 1]] * 2
+
+
+def test_log_probability_workspace_holds_what_the_blocks_write(recorder):
+    """Where rows are shared (a join is launched), every part leaves 4 + 2 top_k floats, in whole groups of four; the number of parts follows from
+    the grid.  Sizes around those where it changes: eight turns of 4096 columns, 32 turns, 512 rows; both types, rows on and off the lines."""
+    shared = 0
+    for vocab in (32768, 65504, 65505, 65536, 65537, 98273, 131040, 131041, 131072, 131073, 200000, 262144, 1 << 20, 1 << 22):
+        for n in (1, 2, 170, 171, 255, 256, 257, 511, 512, 513, 3000):
+            for opts in (dict(), dict(dtype=1), dict(ld=vocab + 1, dtype=1, top_k=32), dict(ld=vocab + 1, top_k=5)):
+                got, error, launches, need = recorder("logprobs", n=n, vocab=vocab, **opts)
+                assert got == OK, error
+                assert len(launches) == (2 if "join" in launches[-1]["kernel"] else 1)
+                if len(launches) == 1:
+                    assert launches[0]["grid"][0] == n
+                    continue
+                shared += 1
+                blocks, floats = launches[0]["grid"][0], (4 + 2 * opts.get("top_k", 0) + 3) // 4 * 4
+                assert blocks % n == 0 and 2 <= blocks // n <= 64 and need >= blocks * floats * 4
+    assert shared > 300
+
+
+def test_gradient_workspace_holds_what_the_blocks_write(recorder):
+    """Where each token begins (and the end), the rows by token, two sums a window; the number of windows follows from the join's grid."""
+    for d in (64, 256, 1024, 1088, 8192):
+        for n in (257, 512, 1000, 4096, 4097, 8192, 8193, 16385, 65536, 100000):
+            for V in (64, 32000, 300032):
+                _, _, launches, need = recorder("embed_grad", n=n, d=d, V=V)
+                strips = (d + 1023) // 1024
+                windows = launches[-1]["grid"][0] // strips
+                sorted_chunks = -(-n // 1024) * (257 * 4 + 1024 * 8) if n > 8192 else 0
+                assert windows * 64 >= n and need >= 4 * (V + 1) + sorted_chunks + 8 * n + 2 * windows * d * 4
