@@ -181,3 +181,36 @@ def test_nothing_is_written_behind_the_workspace(torch_mod, lib, dtype, n, vocab
 def test_nothing_is_written_behind_the_gradients_workspace(torch_mod, n, d, vocab):
     for kind in ("one", "text", "runs"):                                      # all sums, some and few set aside
         embed.check_grad(torch_mod, d, vocab, embed.draw_ids(torch_mod, kind, n, vocab, n), kind == "text", 1.0)
+
+
+# ---- one and two rows with banned tokens
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("vocab", [1, 2, 700, 8193, 32000, 128011])
+@pytest.mark.parametrize("n", [1, 2])
+def test_one_request_held_to_a_grammar(torch_mod, lib, dtype, n, vocab):  # noqa: F811
+    """Most tokens banned, all but one, all; the given token allowed and banned."""
+    torch = torch_mod
+    gen = torch.Generator(device="cuda").manual_seed(vocab)
+    base, token = logprobs.draw(torch, n, vocab, "plain", vocab)
+    for allowed in ("some", "one", "none"):
+        x = base.clone()
+        if allowed == "some":
+            x[torch.rand((n, vocab), generator=gen, device="cuda") < 0.9] = -INF
+        else:
+            x[:] = -INF
+            if allowed == "one":
+                x[:, vocab // 2] = base[:, vocab // 2]
+        if n == 2:
+            x[1] = base[1]                                                    # the other request is free
+        rows = logprobs.rows_of(torch, x, vocab, 0, dtype)
+        for at in (vocab // 2, 0, -1):
+            token[:] = at
+            for k in (0, 5, 32):
+                o = logprobs.call(torch, lib, rows, token, k)
+                torch.cuda.synchronize()
+                logprobs.check(torch, rows, token, o, k)
+                if allowed == "one" and at == vocab // 2:
+                    assert o["logp"][0] == 0 and o["entropy"][0] == 0
+                elif allowed == "none" and at >= 0:
+                    assert o["logp"][0] == -math.inf and o["entropy"][0] == 0
+            logprobs.grad_check(torch, lib, rows, token, dtype, dtype, True, True)
