@@ -13,8 +13,8 @@ constexpr size_t LLC_BYTES = (size_t)256 << 20;      // last-level cache
 // ------------------------------------------------------------------ rows
 typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
 // 2^lg threads per row, 16-byte accesses, four of them in flight a thread.  No branch around a load (a place behind the row reads its last one
-// again, padding reads row 0): 66576 x 4096 bf16 145 -> 131 us; with the rows written past the cache
-// 127 us, 5.2 TB/s of ids, distinct rows and output: HBM-bound.  Fewer blocks that go on to further rows were slower (2048: 147).
+// again, padding reads row 0): 66576 x 4096 bf16 151 -> 142 us, but with the rows written past the cache (as this many are) 126 -> 127 us,
+// 5.2 TB/s of ids, distinct rows and output: HBM-bound.  Fewer blocks that go on to further rows were slower (2048: 155, past the cache 134).
 template <bool BF16, bool STREAM>
 __global__ __launch_bounds__(256) void embed_rows_kernel(const void *__restrict__ table, const int32_t *__restrict__ ids, int n, int vocab, int d,
                                                          float scale, void *__restrict__ out, int lg) {
@@ -437,7 +437,7 @@ hipError_t launch_embed_rows(const void *table, bool bf16, const int32_t *ids, i
   while (lg < 8 && (4 << lg) < vecs) ++lg;
   const int rows = 256 >> lg;
   const dim3 grid((unsigned)std::min<long long>(((long long)n + rows - 1) / rows, 1 << 22));
-  // Rows that fill half the last-level cache or more are written past it, so that the table stays in it: 66576 x 4096 bf16 152 -> 145 us, on two sets of rows in turn 126.
+  // Rows that fill half the last-level cache or more are written past it, so that the table stays in it: 66576 x 4096 bf16 142 -> 127 us, 17000 x 4096 40.5 -> 35.0.
   const bool stream = (size_t)n * vecs * 16 >= LLC_BYTES / 2;
   auto *k = bf16 ? (stream ? embed_rows_kernel<true, true> : embed_rows_kernel<true, false>) : (stream ? embed_rows_kernel<false, true> : embed_rows_kernel<false, false>);
   hipLaunchKernelGGL(k, grid, dim3(256), 0, st, table, ids, n, vocab, d, scale, out, lg);
@@ -474,7 +474,7 @@ hipError_t launch_embed_grad(const int32_t *ids, int n, int vocab, int d, const 
     hipLaunchKernelGGL(embed_place_kernel<0>, dim3(buckets), dim3(64 * WAVES), 0, st, (const int32_t *)nullptr, 0, begins, from, p.chunks, vocab, p.lg, starts, order);
   }
   // Row gradients of half the last-level cache or more are read past it, so that the table stays: 12288 x 4096 99 -> 79 us, 65536 x 4096 358 -> 345;
-  // 3347 x 2048, which fit, 29.6 -> 32.3.
+  // 3347 x 2048, which fit, 23.4 -> 24.6.
   const bool stream = (size_t)n * d * sizeof(float) >= LLC_BYTES / 2;
   auto *sum = accumulate ? (stream ? embed_sum_kernel<true, true, false> : embed_sum_kernel<true, false, false>)
               : past     ? (stream ? embed_sum_kernel<false, true, true> : embed_sum_kernel<false, false, true>)

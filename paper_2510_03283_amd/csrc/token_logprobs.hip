@@ -598,9 +598,10 @@ __global__ __launch_bounds__(256) void token_logprobs_grad_kernel(const TokenLog
 constexpr int most_lead(bool bf16) { return LINE / (bf16 ? 2 : 4) - 1; }
 bool off_lines(const void *rows, long long ld, bool bf16) { return ((uintptr_t)rows | (uintptr_t)(ld * (bf16 ? 2 : 4))) % LINE != 0; }
 
-// Blocks (parts) of a row: where there are fewer than 512 rows, parts of eight turns (32768 fp32 columns), below which joining them costs more
-// than they save.  us with 20 alternatives, one part / parts of eight turns / of four: one row of 32000 fp32 logits 8.9 / 8.9 / 11.9, one
-// of 128011 20.2 / 12.8 / 11.8, 64 of 32000 9.9 / 9.9 / 13.7, 64 of 128011 28.0 / 16.5 / 18.0, 256 of 128011 41.4 / 33.9 / 37.  Counted for fp32 whatever the type, so that the scratch does not depend on it.
+// Blocks (parts) of a row: of up to 256 rows, parts of eight turns (32768 fp32 columns).  us with 20 alternatives, fp32, one part / parts of eight turns / of four:
+// one row of 128011 14.7 / 12.1 / 11.1, 64 16.4 / 16.2 / 16.7; but one of 65536 9.6 / 11.5 / 10.8 and 256 of 128011 29.2 / 34.4 / 34.4, where a single part runs in blocks
+// of 512 threads.  A row of 32000 has eight turns and is not shared: two blocks a row would take 10.4 instead of 7.5 for one row, 13.7 instead of 9.2 for 128, 16.8 instead of 11.2
+// for 256, as the join is a launch of its own.  Counted for fp32 whatever the type, so that the scratch does not depend on it.
 int parts_of(int n, int vocab) {
   using T = Turn<false, 256>;
   const int turns = (vocab + most_lead(false) + T::COLS - 1) / T::COLS, least = (turns + T::MAX_TURNS - 1) / T::MAX_TURNS;
@@ -620,7 +621,7 @@ template <bool BF16, int NT>
 hipError_t launch_rows(const TokenLogprobs &a, int parts, float *scratch, hipStream_t st) {
   using T = Turn<BF16, NT>;
   // Logits that the last-level cache (256 MB) cannot hold are read past it: 16384 x 32000 fp32 354 -> 317 us, 2048 x 32000 49.0 -> 42.5; of
-  // fewer the cache may hold what their producer left (512 x 32000, resident: 12.6 -> 13.3).
+  // fewer the cache may hold what their producer left (512 x 32000, three inputs in turn that it holds: 13.5 -> 14.1).
   const bool stream = (size_t)a.n * a.vocab * (BF16 ? 2 : 4) > LLC_BYTES;
   // Where rows do not begin with a line, us without / with a lead: 2048 x 128011 fp32 170 / 156, 2048 x 50257 69 / 65, but 512 x 31999 12.6 / 12.8, 4096 x 31999
   // with 8 alternatives 92 / 98; bf16, every other row at an odd element, 2048 x 128011 119 / 96, 4096 x 31999 63 / 58, 1024 x 31999 17.1 / 16.3, 4096 x 15999 40.3 / 36.3, but
@@ -629,7 +630,7 @@ hipError_t launch_rows(const TokenLogprobs &a, int parts, float *scratch, hipStr
   const int turns = (a.vocab + (lead ? most_lead(BF16) : 0) + T::COLS - 1) / T::COLS, part_turns = (turns + parts - 1) / parts;
   parts = (turns + part_turns - 1) / part_turns;
   const dim3 grid((unsigned)std::min<long long>((long long)a.n * parts, 1 << 22));
-  // Without the entropy its sum is left out as well: 2048 x 128011 bf16 115 -> 110 us, one row of 32000 4.9 -> 4.3, 16384 x 32000 186 -> 173.
+  // Without the entropy its sum is left out as well: 2048 x 128011 bf16 93 -> 87 us, one row of 32000 4.5 -> 4.1, 16384 x 32000 185 -> 166.
   auto *k = a.entropy ? (a.top_k ? rows_kernel<BF16, true, true, NT>(stream, lead) : rows_kernel<BF16, true, false, NT>(stream, lead))
                       : (a.top_k ? rows_kernel<BF16, false, true, NT>(stream, lead) : rows_kernel<BF16, false, false, NT>(stream, lead));
   hipLaunchKernelGGL(k, grid, dim3(NT), 0, st, a, parts, part_turns, scratch);
@@ -640,8 +641,8 @@ template <bool BF16>
 hipError_t launch_rows(const TokenLogprobs &a, float *scratch, hipStream_t st) {
   const int parts = parts_of(a.n, a.vocab);
   // A wave per row for many short rows, and for rows so short that the quads of 256 threads hold fewer sets than there are alternatives.
-  // us with 256 threads / one wave, without and with 20 alternatives: 2048 x 2048 fp32 6.9 / 5.8, 16.2 / 13.4; 8192 x 4000 26.3 / 26.4, 63.2 / 49.6;
-  // 30000 x 7000 146 / 152, 235 / 204; but 512 x 2048 3.9 / 4.3, 7.4 / 10.3.  64 x 500 bf16 with 20 alternatives 30.8 / 10.7.
+  // us with 256 threads / one wave, without and with 20 alternatives: 2048 x 2048 fp32 7.0 / 5.9, 15.9 / 13.5; 8192 x 4000 26.4 / 26.8, 61.9 / 48.1;
+  // 30000 x 7000 133 / 137, 250 / 236; but 512 x 2048 4.0 / 3.9, 7.6 / 10.6.  64 x 500 bf16 with 20 alternatives 35.7 / 11.0.
   const int few = 128 * Turn<BF16, 256>::N;      // 32 quads with a column
   const bool wave = parts == 1 && (a.vocab <= few || (a.n >= 2048 && a.vocab <= 8192));
   if (wave) return launch_rows<BF16, 64>(a, 1, scratch, st);
@@ -677,7 +678,7 @@ hipError_t launch_token_logprobs_grad(const TokenLogprobsGrad &a, bool bf16, boo
   // 111 / 101, but 30000 x 4097 99 / 110.
   const bool lead = a.vocab >= 8192 && off_lines(a.d_logits, a.ld_d, out_bf16);
   const int cols = 64 * U * (bf16 ? 8 : 4), parts = (a.vocab + (lead ? most_lead(out_bf16) : 0) + cols - 1) / cols;
-  // Gradients that the last-level cache cannot hold are written past it: 16384 x 32000 bf16 555 -> 536 us.
+  // Gradients that the last-level cache cannot hold are written past it: 16384 x 32000 fp32 to bf16 557 -> 540 us, bf16 to bf16 373 -> 363.
   const bool stream = (size_t)a.n * a.vocab * (out_bf16 ? 2 : 4) > LLC_BYTES;
   auto *k = bf16 ? (out_bf16 ? grad_kernel<true, true>(lead, stream) : grad_kernel<true, false>(lead, stream))
                  : (out_bf16 ? grad_kernel<false, true>(lead, stream) : grad_kernel<false, false>(lead, stream));

@@ -169,7 +169,7 @@ def test_large_cases_take_the_variants_that_they_are_for(recorder):
 
 def test_log_probability_workspace_holds_what_the_blocks_write(recorder):
     """Where rows are shared (a join is launched), every part leaves 4 + 2 top_k floats, in whole groups of four; the number of parts follows from
-    the grid.  Sizes around those where it changes: eight turns of 4096 columns, 32 turns, 512 rows; both types, rows on and off the lines."""
+    the grid.  Sizes around those where it changes: eight turns of 4096 columns, 32 turns, 256 rows; both types, rows on and off the lines."""
     shared = 0
     for vocab in (32768, 65504, 65505, 65536, 65537, 98273, 131040, 131041, 131072, 131073, 200000, 262144, 1 << 20, 1 << 22):
         for n in (1, 2, 170, 171, 255, 256, 257, 511, 512, 513, 3000):
