@@ -340,8 +340,9 @@ int mace_embed_tokens_grad(mace_handle_t h, const int32_t *token_ids, int32_t n,
  * A logit of -inf bans its token: probability 0, never listed.  The lowest finite value is an ordinary logit.  A row with nothing but
  * banned tokens: logp -inf, entropy 0, row_stats (-inf, 0).  A NaN or +inf among the vocab columns of a row: its outputs are
  * NaN (logp of padding 0) and its ids -1.  Statistics are fp32 whatever the logits' type, added in an order that depends on the sizes
- * and on the rows' alignment alone.  workspace: mace_token_logprobs_workspace_bytes(h, n, vocab, top_k) bytes, 256-byte aligned, nothing of it read before it
- * is written.  Outputs and workspace overlap neither an input nor each other. */
+ * and on the rows' alignment alone.  workspace: mace_token_logprobs_workspace_bytes(h, n, vocab, top_k) bytes for the n of the call
+ * (fewer rows can need more: they are shared between blocks), 256-byte aligned, nothing of it read before it is written.  Outputs and
+ * workspace overlap neither an input nor each other, judged from first to last element: columns behind vocab belong to their rows. */
 size_t mace_token_logprobs_workspace_bytes(mace_handle_t h, int32_t n, int32_t vocab, int32_t top_k);
 int mace_token_logprobs(mace_handle_t h, const void *logits, int32_t dtype, int32_t n, int32_t vocab, int64_t ld,
                         const int32_t *token_ids, int32_t top_k, float *logp, float *entropy, float *row_stats, int32_t *top_ids,
@@ -352,8 +353,9 @@ int mace_token_logprobs(mace_handle_t h, const void *logits, int32_t dtype, int3
  * logits, dtype, n, vocab, ld, token_ids as above; row_stats and entropy as mace_token_logprobs wrote them for the same logits.
  * d_logp (needs token_ids) and d_entropy (needs entropy) device fp32 [n], at least one of them.  d_logits device, d_dtype MACE_F32 or
  * MACE_BF16 (rounded once), n rows ld_d apart, columns behind vocab left as they are; it may be logits itself (same type and
- * stride) and overlaps nothing else.  Banned tokens have p_j = 0, so gradient 0, or g where the given token is banned.  Rows with
- * nothing but banned tokens and rows whose two weights are 0 (padding counts as g = 0) have gradient 0, the last whatever their
+ * stride) and overlaps nothing else, judged from first to last element (gradient rows between the rows of logits are refused).
+ * Banned tokens have p_j = 0, so gradient 0, or g where the given token is banned.  Rows with nothing but banned tokens and rows
+ * whose two weights are 0 (padding counts as g = 0) have gradient 0, the last whatever their
  * logits hold.  No workspace; one launch. */
 int mace_token_logprobs_grad(mace_handle_t h, const void *logits, int32_t dtype, int32_t n, int32_t vocab, int64_t ld,
                              const int32_t *token_ids, const float *row_stats, const float *entropy, const float *d_logp,

@@ -196,3 +196,18 @@ def test_gradient_workspace_holds_what_the_blocks_write(recorder):
                 windows = launches[-1]["grid"][0] // strips
                 sorted_chunks = -(-n // 1024) * (257 * 4 + 1024 * 8) if n > 8192 else 0
                 assert windows * 64 >= n and need >= 4 * (V + 1) + sorted_chunks + 8 * n + 2 * windows * d * 4
+
+
+def test_rows_between_rows_are_refused(recorder):
+    """Logits and gradient as the two halves of one wide buffer: no element is shared, but their extents cross."""
+    wide = dict(vocab=1024, ld=2048, ld_d=2048, d_dtype=0, same="logits,d_logits", offset=4096)
+    assert recorder("logprobs_grad", **wide)[0] == INVALID
+    assert recorder("logprobs_grad", **{**wide, "n": 1})[0] == OK              # one row: beside each other
+    assert recorder("logprobs_grad", **{**wide, "n": 20, "offset": 4 * (19 * 2048 + 1024)})[0] == OK      # behind the last of 20 rows
+
+
+def test_log_probability_workspace_of_fewer_rows_can_be_larger(recorder):
+    """Up to 256 rows are shared between blocks, so a size is that of its own number of rows only; too small a one is refused."""
+    few, many = (recorder("logprobs", n=n, vocab=128011, top_k=20)[3] for n in (256, 257))
+    assert few > many
+    assert recorder("logprobs", n=256, vocab=128011, top_k=20, work=many)[0] == SMALL
