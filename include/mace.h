@@ -361,6 +361,96 @@ int mace_token_logprobs_grad(mace_handle_t h, const void *logits, int32_t dtype,
                              const int32_t *token_ids, const float *row_stats, const float *entropy, const float *d_logp,
                              const float *d_entropy, void *d_logits, int32_t d_dtype, int64_t ld_d, void *stream);
 
+/* Rotary positions as models have them that the layer's own embedding (half layout, whole head) does not cover, and for contexts longer than
+ * the trained one; the layer calls are not affected.
+ * mace_rotary_frequencies (host, pure): rot_dim / 2 frequencies in 64 bits,
+ *   f_i = theta^(-2i/rot_dim),  inv_freq[i] = f_i (g_i + (1 - g_i) / factor),  g_i = clamp((original_len f_i / 2 pi - slow) / (fast - slow), 0, 1)
+ * frequencies that turn at most `slow` times over the trained length original_len are divided by factor, those that turn at least
+ * `fast` times stay.  original_len = 0: all are divided (g = 0, slow and fast unused); factor = 1: plain frequencies.  rot_dim even, 2..256.
+ * mace_rotary turns the first rot_dim columns (even, <= head_dim) of n_heads heads in each of n rows,
+ *   out[a] = magnitude (x[a] cos t - x[b] sin t),  out[b] = magnitude (x[b] cos t + x[a] sin t),  t = positions[r] inv_freq[i]
+ * (a, b) = (i, i + rot_dim / 2), or (2 i, 2 i + 1) where interleaved != 0; columns of a head behind rot_dim are copied.  inverse != 0: t is
+ * -positions[r] inv_freq[i], which is the gradient (the transposed map).  Angles, sine and cosine are formed in 64 bits, the products in fp32, rounded once.
+ *   x, out     device io_dtype, n rows of n_heads * head_dim columns (queries and keys beside each other: n_heads = Hq + Hkv) that lie
+ *              ld_x, ld_out elements apart; columns behind them are neither read nor written.  Aligned to their elements (16-byte aligned rows and
+ *              rot_dim / 2 a multiple of 16 bytes run fastest).  out may be x (same stride); else they do not overlap, judged from first to last element
+ *   positions  device int32 [n], any value;  inv_freq  device fp64 [rot_dim / 2], any finite values of magnitude up to 2^19;  magnitude finite;  n_heads 1..4096
+ * No workspace; one launch.  The device of mace_create must be current (MACE_INVALID_ARG otherwise; so for the calls below). */
+int mace_rotary_frequencies(int32_t rot_dim, double theta, double factor, int32_t original_len, double slow, double fast, double *inv_freq);
+int mace_rotary(mace_handle_t h, const void *x, int64_t ld_x, const int32_t *positions, const double *inv_freq, int32_t rot_dim, int32_t interleaved,
+                double magnitude, int32_t inverse, int32_t n, int32_t n_heads, void *out, int64_t ld_out, void *stream);
+
+/* Paged KV cache in 4 bits: a little more than a quarter of the bytes of mace_kv_cache_t in bf16.  k, v: device
+ * [num_blocks, n_kv_heads, block_size, head_dim / 2], two values a byte, the even one in the low half; a value is sign, two bits of exponent, one of mantissa:
+ * 0, 1/2, 1, 3/2, 2, 3, 4, 6.  k_scale, v_scale: device [num_blocks, n_kv_heads, block_size, head_dim / 32], one byte b for 32 neighbours of a head, 2^(b - 127);
+ * 255, with codes of 0 only, is NaN.  weight (fp32) and position (int32), [num_blocks, n_kv_heads, block_size], both optional: the attention that each token of each head has been
+ * given, and its position in its request; mace_kv4_evict needs both.  block_size is a power of two (1..256); fewer than 2^31 tokens and 2^32 rows of
+ * heads.  k and v 16-byte aligned, the others 4-byte.  The arrays do not overlap. */
+typedef struct {
+  void *k, *v, *k_scale, *v_scale;
+  float *weight;
+  int32_t *position;
+  int64_t num_blocks;
+  int32_t block_size;
+} mace_kv4_cache_t;
+
+/* Round n rows k_new, v_new (device io_dtype, [n, n_kv_heads * head_dim], rows ld_k, ld_v elements apart, 16-byte aligned) to 4 bits and scatter them into
+ * the cache.  slot_mapping: device int32 [n] (slot_heads = 1), or [n, n_kv_heads] (slot_heads = n_kv_heads) where the heads of a row lie at different places, as behind
+ * an eviction to budgets of their own.  -1 or slots out of range are skipped; two rows of a call do not share a slot of a head (what it then holds is unspecified).
+ * A group of 32 with largest magnitude M takes the scale 2^e, e = floor(log2 M) - 2, plus 1 where M > 7 * 2^e, within -124..125, so that no
+ * value is off by more than half of its own step; values go to the nearest, ties to the even code.  A group with a NaN or an infinity becomes NaN.
+ * weight (if the cache has it) becomes 0, position (if it has it) positions[r], device int32 [n], in 0..2^30 - 1. */
+int mace_kv4_append(mace_handle_t h, const mace_kv4_cache_t *cache, const void *k_new, int64_t ld_k, const void *v_new, int64_t ld_v,
+                    const int32_t *slot_mapping, int32_t slot_heads, const int32_t *positions, int32_t n, void *stream);
+
+/* The values that the cache holds at these slots, as rows k_out, v_out [n, n_kv_heads * head_dim] (device io_dtype, 16-byte aligned; exact in either type).  slot_mapping
+ * as above; a slot out of range yields zeros, and a slot may occur more than once. */
+int mace_kv4_gather(mace_handle_t h, const mace_kv4_cache_t *cache, const int32_t *slot_mapping, int32_t slot_heads, int32_t n, void *k_out, void *v_out,
+                    void *stream);
+
+/* Attention over the 4-bit cache: decode rows, rows of a draft to be verified, pieces of prompts behind a cached context.  Request r has the rows
+ * q_offsets[r] .. q_offsets[r + 1] - 1 of q (device int32 [n_req + 1]; NULL: one row a request, n_rows = n_req and max_rows = 1).  Their keys and values are in the cache
+ * already, behind the context_lens[r] tokens that were there before: row i of a request (from 0) attends to its first context_lens[r] + i + 1 tokens, token t being at place
+ * t % block_size of block block_tables[r, t / block_size].
+ *   q             device io_dtype, n_rows rows of n_q_heads * head_dim columns ld_q apart (16-byte aligned rows);  out likewise, ld_out apart
+ *   block_tables  device int32 [n_req, max_blocks_per_req]
+ *   context_lens  device int32 [n_req] (len_heads = 1) or [n_req, n_kv_heads] (len_heads = n_kv_heads)
+ *   max_context, max_rows  bounds of context_lens and of a request's rows; the launches and the workspace go by them alone, so a captured call may be replayed with
+ *                 other lengths, tables and offsets.  Values beyond them, negative ones and ones that the tables have no room for are cut to what fits
+ *   scale         of the products q . k (usually head_dim^-1/2)
+ *   lse           fp32 [n_rows, n_q_heads], optional: log sum exp of the row's scaled products
+ *   add_weight    != 0: for every token that a row attends to, the probabilities summed over the rows of the request and the query heads of the kv head are added to
+ *                 cache->weight.  The bits are a function of the inputs, except in blocks that requests of the call share: there the requests' sums arrive in any order
+ * Rows of q and out that no request has are neither read nor written.  Tokens of blocks outside the cache are left out; a row without any token has out 0 and
+ * lse -inf.  What lies behind a request's last token in its blocks is never used, whatever it holds.  A NaN in a key makes the rows that attend to it NaN, in a value
+ * their 32 columns.
+ * Precision: codes and scales are exact; q is exact; probabilities are rounded to bf16 before the product with V for bf16 models and carry 24 bits for fp32 ones; all
+ * sums are fp32; out is rounded once.  workspace: mace_kv4_attention_workspace_bytes for the sizes of the call (other sizes can need more or less), 256-byte aligned,
+ * nothing of it read before it is written.  Outputs and workspace overlap neither an input nor each other, judged from first to last element.
+ * n_req, max_rows <= 65535, n_req * max_rows <= 2^24, max_context <= 2^26. */
+size_t mace_kv4_attention_workspace_bytes(mace_handle_t h, int32_t n_req, int32_t max_rows, int32_t max_context);
+int mace_kv4_attention(mace_handle_t h, const mace_kv4_cache_t *cache, const void *q, int64_t ld_q, const int32_t *q_offsets, int32_t n_req, int32_t n_rows,
+                       int32_t max_rows, const int32_t *block_tables, int32_t max_blocks_per_req, const int32_t *context_lens, int32_t len_heads,
+                       int32_t max_context, float scale, int32_t add_weight, void *out, int64_t ld_out, float *lse, void *workspace, size_t workspace_bytes,
+                       void *stream);
+
+/* Cut requests to a budget of tokens for every kv head (Section 4.3, "Decode KV cache pruning"; the budgets may be those of mace_kv_head_budget), by the
+ * attention that the tokens have been given.  Of the context_lens tokens of a head, new_lens[r, head] = min(context_lens, max(budgets[r, head], 0)) stay, those of highest
+ * rank: positions below n_sink (the lower the higher), then positions from seq_lens[r] - n_recent on (the newer the higher), then larger weight; on ties the lower
+ * token.  (Weights that are negative or NaN count as 0; tokens of blocks outside the cache rank last.)
+ * Tokens that stay in front of new_lens remain where they are; the others that stay move into the places of those that go, in order: the i-th place from the front gets the
+ * i-th token from the front.  Codes, scales, weight and position move; places from new_lens on keep what they held.  The order of tokens does not
+ * matter to the attention: keys carry their rotary position.
+ *   context_lens  device int32 [n_req] or [n_req, n_kv_heads] (len_heads as above), at most max_context (larger ones are cut);  budgets  device int32 [n_req, n_kv_heads]
+ *   seq_lens      device int32 [n_req]: tokens that the request has had in all, gone ones included; may be NULL where n_recent is 0
+ *   new_lens      device int32 [n_req, n_kv_heads]; may be context_lens itself where len_heads = n_kv_heads
+ * A block belongs to one request of the call, and to one place of its table: requests that share a prefix copy it first.
+ * workspace: mace_kv4_evict_workspace_bytes, 256-byte aligned, nothing of it read before it is written.  Limits as above. */
+size_t mace_kv4_evict_workspace_bytes(mace_handle_t h, int32_t n_req, int32_t max_context);
+int mace_kv4_evict(mace_handle_t h, const mace_kv4_cache_t *cache, const int32_t *block_tables, int32_t n_req, int32_t max_blocks_per_req,
+                   const int32_t *context_lens, int32_t len_heads, int32_t max_context, const int32_t *seq_lens, const int32_t *budgets, int32_t n_sink,
+                   int32_t n_recent, int32_t *new_lens, void *workspace, size_t workspace_bytes, void *stream);
+
 /* AdamW step (decoupled weight decay) on one tensor of n elements: the optimizer step that turns
  * the gradients of an iteration into the weights the next iteration sees (Section 2.1).  The paper
  * names no optimizer; AdamW is the reading.  step counts from 1.

@@ -23,6 +23,8 @@ EXPORTS = [
     "mace_set_option", "mace_launch_plan", "mace_next_token_logits_static", "mace_gemm_bf16",
     "mace_embed_tokens", "mace_embed_grad_workspace_bytes", "mace_embed_tokens_grad", "mace_token_logprobs_workspace_bytes",
     "mace_token_logprobs", "mace_token_logprobs_grad",
+    "mace_rotary_frequencies", "mace_rotary", "mace_kv4_append", "mace_kv4_gather", "mace_kv4_attention_workspace_bytes", "mace_kv4_attention",
+    "mace_kv4_evict_workspace_bytes", "mace_kv4_evict",
 ]
 MACE_OPT_HEAD_TWO_PASS, MACE_OPT_SINGLE_STREAM, MACE_OPT_DECODE_CHUNK = 1, 2, 3
 
@@ -58,6 +60,11 @@ class LoraGradsT(C.Structure):
 
 class KvCacheT(C.Structure):
     _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("num_blocks", C.c_int64), ("block_size", C.c_int32)]
+
+
+class Kv4CacheT(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p), ("weight", C.c_void_p), ("position", C.c_void_p),
+                ("num_blocks", C.c_int64), ("block_size", C.c_int32)]
 
 
 class BatchT(C.Structure):
@@ -161,6 +168,23 @@ def load():
     lib.mace_token_logprobs.restype = C.c_int
     lib.mace_token_logprobs_grad.argtypes = [vp, vp, i32, i32, i32, i64, vp, vp, vp, vp, vp, vp, i32, i64, vp]
     lib.mace_token_logprobs_grad.restype = C.c_int
+    f64 = C.c_double
+    lib.mace_rotary_frequencies.argtypes = [i32, f64, f64, i32, f64, f64, vp]
+    lib.mace_rotary_frequencies.restype = C.c_int
+    lib.mace_rotary.argtypes = [vp, vp, i64, vp, vp, i32, i32, f64, i32, i32, i32, vp, i64, vp]
+    lib.mace_rotary.restype = C.c_int
+    lib.mace_kv4_append.argtypes = [vp, C.POINTER(Kv4CacheT), vp, i64, vp, i64, vp, i32, vp, i32, vp]
+    lib.mace_kv4_append.restype = C.c_int
+    lib.mace_kv4_gather.argtypes = [vp, C.POINTER(Kv4CacheT), vp, i32, i32, vp, vp, vp]
+    lib.mace_kv4_gather.restype = C.c_int
+    lib.mace_kv4_attention_workspace_bytes.argtypes = [vp, i32, i32, i32]
+    lib.mace_kv4_attention_workspace_bytes.restype = sz
+    lib.mace_kv4_attention.argtypes = [vp, C.POINTER(Kv4CacheT), vp, i64, vp, i32, i32, i32, vp, i32, vp, i32, i32, f32, i32, vp, i64, vp, vp, sz, vp]
+    lib.mace_kv4_attention.restype = C.c_int
+    lib.mace_kv4_evict_workspace_bytes.argtypes = [vp, i32, i32]
+    lib.mace_kv4_evict_workspace_bytes.restype = sz
+    lib.mace_kv4_evict.argtypes = [vp, C.POINTER(Kv4CacheT), vp, i32, i32, vp, i32, i32, vp, vp, i32, i32, vp, vp, sz, vp]
+    lib.mace_kv4_evict.restype = C.c_int
     _lib = lib
     return lib
 
@@ -199,6 +223,7 @@ def mace_create(d_model, n_q_heads, n_kv_heads, head_dim, d_ff, vocab, rms_eps, 
     _check(load().mace_create(C.byref(h), C.byref(m)), "mace_create")
     h.table_shape, h.io_dtype = (vocab, d_model), torch.bfloat16 if io_dtype == MACE_BF16 else torch.float32
     h.device = torch.cuda.current_device()
+    h.q_heads, h.kv_heads, h.head_dim = n_q_heads, n_kv_heads, head_dim
     return h
 
 
@@ -446,6 +471,112 @@ def mace_token_logprobs_grad(h, logits, row_stats, d_logits, token_ids=None, d_l
                                            _tensor(h, row_stats, "row_stats", f, (n, 2)), _tensor(h, entropy, "entropy", f, (n,)),
                                            _tensor(h, d_logp, "d_logp", f, (n,)), _tensor(h, d_entropy, "d_entropy", f, (n,)), q, d_dtype, ld_d,
                                            _stream(stream)), "mace_token_logprobs_grad")
+
+
+def mace_rotary_frequencies(rot_dim: int, theta: float, factor: float = 1.0, original_len: int = 0, slow: float = 1.0, fast: float = 32.0):
+    """Host-side rotary frequencies, scaled for contexts `factor` times the trained length; returns a numpy float64 array."""
+    import numpy as np
+    out = np.empty(max(rot_dim // 2, 1), dtype=np.float64)
+    _check(load().mace_rotary_frequencies(int(rot_dim), float(theta), float(factor), int(original_len), float(slow), float(fast), C.c_void_p(out.ctypes.data)),
+           "mace_rotary_frequencies")
+    return out
+
+
+def _head_rows(h, t, name: str, heads: int):
+    """(pointer, rows, row stride) of a matrix in the handle's type whose rows begin with `heads` heads, columns adjacent."""
+    if t.dim() != 2 or t.dtype != h.io_dtype or t.get_device() != h.device or t.shape[1] < heads * h.head_dim or (t.stride(1) != 1 and t.shape[1] > 1):
+        raise MaceError(f"{name}: a matrix of {h.io_dtype} with adjacent columns, at least {heads} heads of {h.head_dim} of them, on cuda:{h.device} is wanted, "
+                        f"got {t.dtype} {tuple(t.shape)} with strides {t.stride()} on {t.device}")
+    n = t.shape[0]
+    return t.data_ptr(), n, t.stride(0) if n > 1 else max(t.stride(0), t.shape[1])
+
+
+def mace_rotary(h, x, positions, inv_freq, out, n_heads: int, interleaved=False, magnitude: float = 1.0, inverse=False, stream=None):
+    """out = the first n_heads heads of every row of x turned by positions [n] and inv_freq [rot_dim / 2] (fp64, device); out may be x."""
+    p, n, ld_x = _head_rows(h, x, "x", n_heads)
+    q, n_out, ld_out = _head_rows(h, out, "out", n_heads)
+    if n_out != n:
+        raise MaceError(f"out: {n_out} rows for {n} rows of x")
+    _check(load().mace_rotary(h, p, ld_x, _tensor(h, positions, "positions", torch.int32, (n,)), _tensor(h, inv_freq, "inv_freq", torch.float64, inv_freq.shape),
+                              2 * inv_freq.numel(), int(bool(interleaved)), float(magnitude), int(bool(inverse)), n, int(n_heads), q, ld_out, _stream(stream)), "mace_rotary")
+
+
+def kv4_cache_struct(k, v, k_scale, v_scale, weight=None, position=None) -> Kv4CacheT:
+    """Cache in 4 bits from its arrays: k, v uint8 [blocks, kv heads, block size, head_dim / 2], scales uint8 [.., head_dim / 32], weight fp32 and
+    position int32 [blocks, kv heads, block size]."""
+    blocks, heads, size, half = k.shape
+    scales, places = (blocks, heads, size, half // 16), (blocks, heads, size)
+    for name, t, dtype, shape in (("k", k, torch.uint8, k.shape), ("v", v, torch.uint8, k.shape), ("k_scale", k_scale, torch.uint8, scales),
+                                  ("v_scale", v_scale, torch.uint8, scales), ("weight", weight, torch.float32, places), ("position", position, torch.int32, places)):
+        if t is not None and (t.dtype != dtype or t.shape != shape or not t.is_contiguous() or t.device != k.device):
+            raise MaceError(f"{name}: a contiguous tensor of {dtype} {tuple(shape)} on {k.device} is wanted, got {t.dtype} {tuple(t.shape)} on {t.device}")
+    c = Kv4CacheT(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), weight.data_ptr() if weight is not None else None,
+                  position.data_ptr() if position is not None else None, blocks, size)
+    c.shape, c.device, c.arrays = (heads, 2 * half), k.get_device(), (k, v, k_scale, v_scale, weight, position)          # (the arrays live as long as the struct)
+    return c
+
+
+def _kv4(h, cache: Kv4CacheT):
+    if cache.shape != (h.kv_heads, h.head_dim) or cache.device != h.device:
+        raise MaceError(f"cache: {h.kv_heads} kv heads of {h.head_dim} on cuda:{h.device} are wanted, got {cache.shape[0]} of {cache.shape[1]} on device {cache.device}")
+    return C.byref(cache)
+
+
+def _per_head(h, t, name: str, n: int):
+    """(pointer, heads) of an int32 array [n] or [n, kv heads]."""
+    heads = 1 if t.dim() == 1 else h.kv_heads
+    return _tensor(h, t, name, torch.int32, (n,) if t.dim() == 1 else (n, heads)), heads
+
+
+def mace_kv4_append(h, cache: Kv4CacheT, k_new, v_new, slot_mapping, positions=None, stream=None):
+    """Rows k_new, v_new [n, >= n_kv_heads * head_dim] (any row stride of whole 16 bytes) rounded to 4 bits, into the slots [n] or [n, kv heads]."""
+    p, n, ld_k = _head_rows(h, k_new, "k_new", h.kv_heads)
+    q, n_v, ld_v = _head_rows(h, v_new, "v_new", h.kv_heads)
+    if n_v != n:
+        raise MaceError(f"v_new: {n_v} rows for {n} rows of k_new")
+    _check(load().mace_kv4_append(h, _kv4(h, cache), p, ld_k, q, ld_v, *_per_head(h, slot_mapping, "slot_mapping", n),
+                                  _tensor(h, positions, "positions", torch.int32, (n,)), n, _stream(stream)), "mace_kv4_append")
+
+
+def mace_kv4_gather(h, cache: Kv4CacheT, slot_mapping, k_out, v_out, stream=None):
+    """Values at the slots [n] or [n, kv heads] as rows k_out, v_out [n, n_kv_heads * head_dim]."""
+    n, shape = slot_mapping.shape[0], (slot_mapping.shape[0], h.kv_heads * h.head_dim)
+    _check(load().mace_kv4_gather(h, _kv4(h, cache), *_per_head(h, slot_mapping, "slot_mapping", n), n, _tensor(h, k_out, "k_out", h.io_dtype, shape),
+                                  _tensor(h, v_out, "v_out", h.io_dtype, shape), _stream(stream)), "mace_kv4_gather")
+
+
+def mace_kv4_attention_workspace_bytes(h, n_req: int, max_rows: int, max_context: int) -> int:
+    return int(load().mace_kv4_attention_workspace_bytes(h, n_req, max_rows, max_context))
+
+
+def mace_kv4_attention(h, cache: Kv4CacheT, q, block_tables, context_lens, out, workspace, max_context: int, q_offsets=None, max_rows: int = 1, lse=None,
+                       scale=None, add_weight=False, stream=None):
+    """Rows q [n, >= n_q_heads * head_dim] over the cached tokens of their requests, into out; context_lens [requests] or [requests, kv heads]."""
+    p, n, ld_q = _head_rows(h, q, "q", h.q_heads)
+    o, n_out, ld_out = _head_rows(h, out, "out", h.q_heads)
+    if n_out != n:
+        raise MaceError(f"out: {n_out} rows for {n} rows of q")
+    n_req, most = block_tables.shape
+    lens, len_heads = _per_head(h, context_lens, "context_lens", n_req)
+    _check(load().mace_kv4_attention(h, _kv4(h, cache), p, ld_q, _tensor(h, q_offsets, "q_offsets", torch.int32, (n_req + 1,)), n_req, n, int(max_rows),
+                                     _tensor(h, block_tables, "block_tables", torch.int32, (n_req, most)), most, lens, len_heads, int(max_context),
+                                     float(h.head_dim ** -0.5 if scale is None else scale), int(bool(add_weight)), o, ld_out,
+                                     _tensor(h, lse, "lse", torch.float32, (n, h.q_heads)), *_workspace(h, workspace), _stream(stream)), "mace_kv4_attention")
+
+
+def mace_kv4_evict_workspace_bytes(h, n_req: int, max_context: int) -> int:
+    return int(load().mace_kv4_evict_workspace_bytes(h, n_req, max_context))
+
+
+def mace_kv4_evict(h, cache: Kv4CacheT, block_tables, context_lens, seq_lens, budgets, new_lens, workspace, max_context: int, n_sink: int = 0,
+                   n_recent: int = 0, stream=None):
+    """Cut every request and kv head to budgets [requests, kv heads] tokens; new_lens [requests, kv heads] may be context_lens itself."""
+    n_req, most = block_tables.shape
+    i32, shape = torch.int32, (n_req, h.kv_heads)
+    lens, len_heads = _per_head(h, context_lens, "context_lens", n_req)
+    _check(load().mace_kv4_evict(h, _kv4(h, cache), _tensor(h, block_tables, "block_tables", i32, (n_req, most)), n_req, most, lens, len_heads, int(max_context),
+                                 _tensor(h, seq_lens, "seq_lens", i32, (n_req,)), _tensor(h, budgets, "budgets", i32, shape), int(n_sink), int(n_recent),
+                                 _tensor(h, new_lens, "new_lens", i32, shape), *_workspace(h, workspace), _stream(stream)), "mace_kv4_evict")
 
 
 def mace_adamw_step(h, param, master, grad, m, v, lr, beta1, beta2, eps, weight_decay, step, stream=None):

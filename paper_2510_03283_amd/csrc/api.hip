@@ -979,6 +979,214 @@ int mace_token_logprobs_grad(mace_handle_t h, const void *logits, int32_t dtype,
   return MACE_OK;
 }
 
+// ---- long contexts on a compressed cache ----
+extern "C++" {
+namespace {
+struct Extent { const void *p; size_t bytes; };
+// Whether one of the written buffers overlaps a read one or another written one (null or empty buffers do not).
+template <size_t W, size_t R>
+bool overlaps(const Extent (&written)[W], const Extent (&read)[R]) {
+  auto meet = [](const Extent &a, const Extent &b) { return a.p && b.p && a.bytes && b.bytes && overlap(a.p, a.bytes, b.p, b.bytes); };
+  for (size_t i = 0; i < W; ++i) {
+    for (const Extent &r : read) if (meet(written[i], r)) return true;
+    for (size_t j = i + 1; j < W; ++j) if (meet(written[i], written[j])) return true;
+  }
+  return false;
+}
+// From the first to the last element of rows of `cols` elements that lie ld apart.
+size_t strided_bytes(int32_t n, int64_t cols, int64_t ld, size_t elem) { return n > 0 ? ((size_t)(n - 1) * (size_t)ld + (size_t)cols) * elem : 0; }
+bool misaligned(std::initializer_list<const void *> ps, uintptr_t by) {
+  for (const void *p : ps) if ((uintptr_t)p & (by - 1)) return true;
+  return false;
+}
+}  // namespace
+}
+
+int mace_rotary_frequencies(int32_t rot_dim, double theta, double factor, int32_t original_len, double slow, double fast, double *inv_freq) {
+  if (!inv_freq) return fail(MACE_INVALID_ARG, "mace_rotary_frequencies: inv_freq is null");
+  if (rot_dim < 2 || rot_dim > 256 || rot_dim % 2) return fail(MACE_BAD_SHAPE, "mace_rotary_frequencies: rot_dim must be even and in 2..256");
+  if (!(theta > 0.0) || !std::isfinite(theta) || !(factor > 0.0) || !std::isfinite(factor) || original_len < 0) return fail(MACE_INVALID_ARG, "mace_rotary_frequencies: theta and factor must be positive and finite, original_len at least 0");
+  if (original_len > 0 && (!std::isfinite(slow) || !std::isfinite(fast) || !(slow < fast))) return fail(MACE_INVALID_ARG, "mace_rotary_frequencies: slow must be below fast");
+  const double two_pi = 6.283185307179586476925;
+  for (int32_t i = 0; i < rot_dim / 2; ++i) {
+    const double f = std::pow(theta, -2.0 * i / rot_dim);
+    const double keep = original_len > 0 ? std::min(std::max((original_len * f / two_pi - slow) / (fast - slow), 0.0), 1.0) : 0.0;
+    inv_freq[i] = f * (keep + (1.0 - keep) / factor);
+  }
+  return MACE_OK;
+}
+
+int mace_rotary(mace_handle_t h, const void *x, int64_t ld_x, const int32_t *positions, const double *inv_freq, int32_t rot_dim, int32_t interleaved,
+                double magnitude, int32_t inverse, int32_t n, int32_t n_heads, void *out, int64_t ld_out, void *stream) {
+  const char *what = "mace_rotary";
+  if (!h) return fail(MACE_INVALID_ARG, "handle is null");
+  const Dims D(h->m);
+  if (n < 0 || (n > 0 && (!x || !positions || !inv_freq || !out))) return fail(MACE_INVALID_ARG, "mace_rotary: bad argument");
+  if (rot_dim < 2 || rot_dim > D.hd || rot_dim % 2) return fail(MACE_BAD_SHAPE, "mace_rotary: rot_dim must be even and in 2..head_dim");
+  if (n_heads < 1 || n_heads > 4096) return fail(MACE_BAD_SHAPE, "mace_rotary: n_heads must be in 1..4096");
+  const int64_t cols = (int64_t)n_heads * D.hd;
+  if (ld_x < cols || ld_out < cols || ld_x > INT32_MAX || ld_out > INT32_MAX) return fail(MACE_BAD_SHAPE, "mace_rotary: a row stride must be at least n_heads * head_dim and below 2^31");
+  if (!std::isfinite(magnitude)) return fail(MACE_INVALID_ARG, "mace_rotary: magnitude must be finite");
+  const size_t es = D.bf ? 2 : 4;
+  if (misaligned({x, out}, es) || misaligned({positions}, 4) || misaligned({inv_freq}, 8)) return fail(MACE_INVALID_ARG, "mace_rotary: pointer not aligned to its elements");
+  if (n == 0) return MACE_OK;
+  const bool in_place = x == out && (ld_x == ld_out || n == 1);
+  const Extent written[] = {{out, strided_bytes(n, cols, ld_out, es)}};
+  const Extent read[] = {{in_place ? nullptr : x, strided_bytes(n, cols, ld_x, es)}, {positions, (size_t)4 * n}, {inv_freq, (size_t)4 * rot_dim}};
+  if (overlaps(written, read)) return fail(MACE_INVALID_ARG, "mace_rotary: out overlaps an input without being the same rows");
+  TRY(check_device(h, what));
+  const Rotary a = {x, out, ld_x, ld_out, positions, inv_freq, n, n_heads, D.hd, rot_dim, magnitude, interleaved != 0, inverse != 0};
+  prof_mark(h, (hipStream_t)stream, T_ROPE);
+  HIP_TRY(launch_rotary(a, D.bf, (hipStream_t)stream), "rotary");
+  prof_mark(h, (hipStream_t)stream, -1);
+  return MACE_OK;
+}
+
+static int check_kv4(const mace_kv4_cache_t *c, const Dims &D, const char *what, Kv4Cache *out) {
+  if (!c || !c->k || !c->v || !c->k_scale || !c->v_scale) return fail(MACE_INVALID_ARG, std::string(what) + ": the cache is null");
+  if (c->block_size <= 0 || c->block_size > 256 || (c->block_size & (c->block_size - 1))) return fail(MACE_INVALID_ARG, std::string(what) + ": block_size must be a power of two in 1..256");
+  if (c->num_blocks <= 0) return fail(MACE_INVALID_ARG, std::string(what) + ": the cache has no blocks");
+  if (c->num_blocks >= (1ll << 32) / ((int64_t)D.Hkv * c->block_size) || c->num_blocks * c->block_size > INT32_MAX) return fail(MACE_BAD_SHAPE, std::string(what) + ": the cache holds 2^31 tokens or 2^32 rows of heads");
+  if (misaligned({c->k, c->v}, 16) || misaligned({c->k_scale, c->v_scale, c->weight, c->position}, 4)) return fail(MACE_INVALID_ARG, std::string(what) + ": k and v must be 16-byte aligned, the other arrays 4-byte");
+  int shift = 0;
+  while ((1 << shift) < c->block_size) ++shift;
+  *out = {(unsigned char *)c->k, (unsigned char *)c->v, (unsigned char *)c->k_scale, (unsigned char *)c->v_scale, c->weight, c->position, (uint32_t)c->num_blocks, shift, D.Hkv, D.hd};
+  return MACE_OK;
+}
+static size_t kv4_tokens(const Kv4Cache &c) { return ((size_t)c.num_blocks * c.Hkv) << c.bshift; }
+#define KV4_EXTENTS(c, tokens) {(c).k, (tokens) * (c).hd / 2}, {(c).v, (tokens) * (c).hd / 2}, {(c).k_scale, (tokens) * (c).hd / 32}, {(c).v_scale, (tokens) * (c).hd / 32}
+
+int mace_kv4_append(mace_handle_t h, const mace_kv4_cache_t *cache, const void *k_new, int64_t ld_k, const void *v_new, int64_t ld_v,
+                    const int32_t *slot_mapping, int32_t slot_heads, const int32_t *positions, int32_t n, void *stream) {
+  const char *what = "mace_kv4_append";
+  if (!h) return fail(MACE_INVALID_ARG, "handle is null");
+  const Dims D(h->m);
+  Kv4Cache c;
+  TRY(check_kv4(cache, D, what, &c));
+  if (n < 0 || (n > 0 && (!k_new || !v_new || !slot_mapping))) return fail(MACE_INVALID_ARG, "mace_kv4_append: bad argument");
+  if (slot_heads != 1 && slot_heads != D.Hkv) return fail(MACE_BAD_SHAPE, "mace_kv4_append: slot_heads must be 1 or n_kv_heads");
+  if (n > 0 && c.position && !positions) return fail(MACE_INVALID_ARG, "mace_kv4_append: a cache with positions needs those of the rows");
+  const int64_t cols = (int64_t)D.Hkv * D.hd;
+  const int step = D.bf ? 8 : 4;
+  if (ld_k < cols || ld_v < cols || ld_k % step || ld_v % step || ld_k > INT32_MAX || ld_v > INT32_MAX) return fail(MACE_BAD_SHAPE, "mace_kv4_append: a row stride must be at least n_kv_heads * head_dim, a multiple of 16 bytes and below 2^31");
+  if ((int64_t)n * cols / 8 > INT32_MAX) return fail(MACE_BAD_SHAPE, "mace_kv4_append: too many rows");
+  if (misaligned({k_new, v_new}, 16) || misaligned({slot_mapping, positions}, 4)) return fail(MACE_INVALID_ARG, "mace_kv4_append: k_new and v_new must be 16-byte aligned, the index arrays 4-byte");
+  if (n == 0) return MACE_OK;
+  const size_t tokens = kv4_tokens(c), es = D.bf ? 2 : 4;
+  const Extent written[] = {KV4_EXTENTS(c, tokens), {c.weight, tokens * 4}, {c.position, tokens * 4}};
+  const Extent read[] = {{k_new, strided_bytes(n, cols, ld_k, es)}, {v_new, strided_bytes(n, cols, ld_v, es)}, {slot_mapping, (size_t)4 * n * slot_heads}, {positions, (size_t)4 * n}};
+  if (overlaps(written, read)) return fail(MACE_INVALID_ARG, "mace_kv4_append: the cache's arrays overlap each other or an input");
+  TRY(check_device(h, what));
+  prof_mark(h, (hipStream_t)stream, T_MISC);
+  HIP_TRY(launch_kv4_append(c, k_new, ld_k, v_new, ld_v, D.bf, slot_mapping, slot_heads, positions, n, (hipStream_t)stream), "kv4 append");
+  prof_mark(h, (hipStream_t)stream, -1);
+  return MACE_OK;
+}
+
+int mace_kv4_gather(mace_handle_t h, const mace_kv4_cache_t *cache, const int32_t *slot_mapping, int32_t slot_heads, int32_t n, void *k_out, void *v_out,
+                    void *stream) {
+  const char *what = "mace_kv4_gather";
+  if (!h) return fail(MACE_INVALID_ARG, "handle is null");
+  const Dims D(h->m);
+  Kv4Cache c;
+  TRY(check_kv4(cache, D, what, &c));
+  if (n < 0 || (n > 0 && (!slot_mapping || !k_out || !v_out))) return fail(MACE_INVALID_ARG, "mace_kv4_gather: bad argument");
+  if (slot_heads != 1 && slot_heads != D.Hkv) return fail(MACE_BAD_SHAPE, "mace_kv4_gather: slot_heads must be 1 or n_kv_heads");
+  const int64_t cols = (int64_t)D.Hkv * D.hd;
+  if ((int64_t)n * cols / 8 > INT32_MAX) return fail(MACE_BAD_SHAPE, "mace_kv4_gather: too many rows");
+  if (misaligned({k_out, v_out}, 16) || misaligned({slot_mapping}, 4)) return fail(MACE_INVALID_ARG, "mace_kv4_gather: k_out and v_out must be 16-byte aligned, slot_mapping 4-byte");
+  if (n == 0) return MACE_OK;
+  const size_t tokens = kv4_tokens(c), out = (size_t)n * cols * (D.bf ? 2 : 4);
+  const Extent written[] = {{k_out, out}, {v_out, out}};
+  const Extent read[] = {KV4_EXTENTS(c, tokens), {slot_mapping, (size_t)4 * n * slot_heads}};
+  if (overlaps(written, read)) return fail(MACE_INVALID_ARG, "mace_kv4_gather: an output overlaps an input or the other output");
+  TRY(check_device(h, what));
+  prof_mark(h, (hipStream_t)stream, T_MISC);
+  HIP_TRY(launch_kv4_gather(c, slot_mapping, slot_heads, n, k_out, v_out, D.bf, (hipStream_t)stream), "kv4 gather");
+  prof_mark(h, (hipStream_t)stream, -1);
+  return MACE_OK;
+}
+
+// Requests, rows of one request and cached tokens that the attention and the eviction take: grid limits, and token numbers that stay below 2^31.
+static bool kv4_sizes_ok(int32_t n_req, int32_t max_rows, int32_t max_context) {
+  return n_req >= 0 && n_req <= 65535 && max_rows >= 1 && max_rows <= 65535 && max_context >= 0 && max_context <= (1 << 26) && (int64_t)n_req * max_rows <= (1 << 24);
+}
+
+size_t mace_kv4_attention_workspace_bytes(mace_handle_t h, int32_t n_req, int32_t max_rows, int32_t max_context) {
+  if (!h || !kv4_sizes_ok(n_req, max_rows, max_context)) return 0;
+  return align_up(std::max<size_t>(kv4_attention_scratch_bytes(n_req, max_rows, max_context, h->m.n_q_heads, h->m.n_kv_heads, h->m.head_dim), 1), 256);
+}
+
+int mace_kv4_attention(mace_handle_t h, const mace_kv4_cache_t *cache, const void *q, int64_t ld_q, const int32_t *q_offsets, int32_t n_req, int32_t n_rows,
+                       int32_t max_rows, const int32_t *block_tables, int32_t max_blocks_per_req, const int32_t *context_lens, int32_t len_heads,
+                       int32_t max_context, float scale, int32_t add_weight, void *out, int64_t ld_out, float *lse, void *workspace, size_t workspace_bytes,
+                       void *stream) {
+  const char *what = "mace_kv4_attention";
+  if (!h) return fail(MACE_INVALID_ARG, "handle is null");
+  const Dims D(h->m);
+  Kv4Cache c;
+  TRY(check_kv4(cache, D, what, &c));
+  if (!kv4_sizes_ok(n_req, max_rows, max_context) || n_rows < 0 || max_blocks_per_req < 0) return fail(MACE_BAD_SHAPE, "mace_kv4_attention: at most 65535 requests of 1..65535 rows (2^24 in all) and 2^26 cached tokens");
+  if (n_req > 0 && n_rows > 0 && (!q || !block_tables || !context_lens || !out)) return fail(MACE_INVALID_ARG, "mace_kv4_attention: bad argument");
+  if (!q_offsets && (max_rows != 1 || n_rows != n_req)) return fail(MACE_INVALID_ARG, "mace_kv4_attention: without q_offsets every request has one row");
+  if (len_heads != 1 && len_heads != D.Hkv) return fail(MACE_BAD_SHAPE, "mace_kv4_attention: len_heads must be 1 or n_kv_heads");
+  if (!std::isfinite(scale)) return fail(MACE_INVALID_ARG, "mace_kv4_attention: scale must be finite");
+  if (add_weight && !c.weight) return fail(MACE_INVALID_ARG, "mace_kv4_attention: the cache has no weights to add to");
+  const int64_t cols = (int64_t)D.Hq * D.hd;
+  const int step = D.bf ? 8 : 4;
+  if (ld_q < cols || ld_out < cols || ld_q % step || ld_out % step || ld_q > INT32_MAX || ld_out > INT32_MAX) return fail(MACE_BAD_SHAPE, "mace_kv4_attention: a row stride must be at least n_q_heads * head_dim, a multiple of 16 bytes and below 2^31");
+  if (misaligned({q, out}, 16) || misaligned({q_offsets, block_tables, context_lens, lse}, 4)) return fail(MACE_INVALID_ARG, "mace_kv4_attention: q and out must be 16-byte aligned, the other arrays 4-byte");
+  if (n_req == 0 || n_rows == 0) return MACE_OK;
+  const size_t need = mace_kv4_attention_workspace_bytes(h, n_req, max_rows, max_context), tokens = kv4_tokens(c), es = D.bf ? 2 : 4;
+  TRY(check_scratch(workspace, workspace_bytes, need, what));
+  const Extent written[] = {{out, strided_bytes(n_rows, cols, ld_out, es)}, {lse, (size_t)4 * n_rows * D.Hq}, {workspace, need}, {add_weight ? c.weight : nullptr, tokens * 4}};
+  const Extent read[] = {KV4_EXTENTS(c, tokens), {q, strided_bytes(n_rows, cols, ld_q, es)}, {q_offsets, (size_t)4 * (n_req + 1)},
+                         {block_tables, (size_t)4 * n_req * max_blocks_per_req}, {context_lens, (size_t)4 * n_req * len_heads}};
+  if (overlaps(written, read)) return fail(MACE_INVALID_ARG, "mace_kv4_attention: an output or the workspace overlaps an input or another output");
+  TRY(check_device(h, what));
+  const Kv4Attention a = {c, q, out, ld_q, ld_out, q_offsets, block_tables, context_lens, n_req, n_rows, max_rows, max_blocks_per_req, len_heads, max_context, D.Hq / D.Hkv,
+                          scale, lse, add_weight != 0};
+  prof_mark(h, (hipStream_t)stream, T_ATTN_DECODE);
+  HIP_TRY(launch_kv4_attention(a, D.bf, workspace, (hipStream_t)stream), "kv4 attention");
+  prof_mark(h, (hipStream_t)stream, -1);
+  return MACE_OK;
+}
+
+size_t mace_kv4_evict_workspace_bytes(mace_handle_t h, int32_t n_req, int32_t max_context) {
+  if (!h || !kv4_sizes_ok(n_req, 1, max_context)) return 0;
+  return align_up(std::max<size_t>(kv4_evict_scratch_bytes(n_req, max_context, h->m.n_kv_heads), 1), 256);
+}
+
+int mace_kv4_evict(mace_handle_t h, const mace_kv4_cache_t *cache, const int32_t *block_tables, int32_t n_req, int32_t max_blocks_per_req,
+                   const int32_t *context_lens, int32_t len_heads, int32_t max_context, const int32_t *seq_lens, const int32_t *budgets, int32_t n_sink,
+                   int32_t n_recent, int32_t *new_lens, void *workspace, size_t workspace_bytes, void *stream) {
+  const char *what = "mace_kv4_evict";
+  if (!h) return fail(MACE_INVALID_ARG, "handle is null");
+  const Dims D(h->m);
+  Kv4Cache c;
+  TRY(check_kv4(cache, D, what, &c));
+  if (!c.weight || !c.position) return fail(MACE_INVALID_ARG, "mace_kv4_evict: the cache needs weights and positions");
+  if (!kv4_sizes_ok(n_req, 1, max_context) || max_blocks_per_req < 0) return fail(MACE_BAD_SHAPE, "mace_kv4_evict: at most 65535 requests and 2^26 cached tokens");
+  if (n_req > 0 && (!block_tables || !context_lens || !budgets || !new_lens || (n_recent > 0 && !seq_lens))) return fail(MACE_INVALID_ARG, "mace_kv4_evict: bad argument");
+  if (len_heads != 1 && len_heads != D.Hkv) return fail(MACE_BAD_SHAPE, "mace_kv4_evict: len_heads must be 1 or n_kv_heads");
+  if (n_sink < 0 || n_recent < 0) return fail(MACE_INVALID_ARG, "mace_kv4_evict: n_sink and n_recent must be at least 0");
+  if (misaligned({block_tables, context_lens, seq_lens, budgets, new_lens}, 4)) return fail(MACE_INVALID_ARG, "mace_kv4_evict: the index arrays must be 4-byte aligned");
+  if (n_req == 0) return MACE_OK;
+  const size_t need = mace_kv4_evict_workspace_bytes(h, n_req, max_context), tokens = kv4_tokens(c), heads = (size_t)4 * n_req * D.Hkv;
+  TRY(check_scratch(workspace, workspace_bytes, need, what));
+  const bool in_place = new_lens == context_lens && len_heads == D.Hkv;
+  const Extent written[] = {KV4_EXTENTS(c, tokens), {c.weight, tokens * 4}, {c.position, tokens * 4}, {new_lens, heads}, {workspace, need}};
+  const Extent read[] = {{block_tables, (size_t)4 * n_req * max_blocks_per_req}, {in_place ? nullptr : context_lens, (size_t)4 * n_req * len_heads},
+                         {seq_lens, (size_t)4 * n_req}, {budgets, heads}};
+  if (overlaps(written, read)) return fail(MACE_INVALID_ARG, "mace_kv4_evict: the cache, new_lens or the workspace overlaps another array");
+  TRY(check_device(h, what));
+  const Kv4Evict a = {c, block_tables, context_lens, seq_lens, budgets, n_req, max_blocks_per_req, len_heads, max_context, n_sink, n_recent, new_lens};
+  prof_mark(h, (hipStream_t)stream, T_MISC);
+  HIP_TRY(launch_kv4_evict(a, workspace, (hipStream_t)stream), "kv4 evict");
+  prof_mark(h, (hipStream_t)stream, -1);
+  return MACE_OK;
+}
+
 int mace_adamw_step(mace_handle_t h, void *param, float *master, const float *grad, float *m, float *v, int64_t n, float lr,
                     float beta1, float beta2, float eps, float weight_decay, int32_t step, void *stream) {
   if (!h || !param || !grad || !m || !v || n < 0) return fail(MACE_INVALID_ARG, "mace_adamw_step: bad argument");

@@ -270,3 +270,52 @@ struct TokenLogprobsGrad {
   void *d_logits;
 };
 hipError_t launch_token_logprobs_grad(const TokenLogprobsGrad &a, bool bf16, bool out_bf16, hipStream_t st);
+
+// ---- rotary.hip ------------------------------------------------------------------------------
+// Heads of n rows (row strides ld_x, ld_out in elements) turned by positions[r] * inv_freq[i], i < rot / 2; see mace_rotary.  out may be x.
+struct Rotary {
+  const void *x;
+  void *out;
+  long long ld_x, ld_out;
+  const int32_t *positions;
+  const double *inv_freq;
+  int n, n_heads, hd, rot;
+  double magnitude;
+  bool interleaved, inverse;
+};
+hipError_t launch_rotary(const Rotary &a, bool bf16, hipStream_t st);
+
+// ---- kv4_cache.hip, kv4_attention.hip, kv4_evict.hip -------------------------------------------
+// Paged cache in 4 bits, see mace_kv4_cache_t.  A token of a kv head has the index (block * Hkv + head) * B + place, below 2^32.
+struct Kv4Cache {
+  unsigned char *k, *v, *k_scale, *v_scale;
+  float *weight;
+  int32_t *position;
+  uint32_t num_blocks;
+  int bshift, Hkv, hd;      // B = 1 << bshift
+};
+// slots [n] or [n, Hkv] (slot_heads = 1 or Hkv)
+hipError_t launch_kv4_append(const Kv4Cache &c, const void *k_new, long long ld_k, const void *v_new, long long ld_v, bool bf16, const int32_t *slots,
+                             int slot_heads, const int32_t *positions, int n, hipStream_t st);
+hipError_t launch_kv4_gather(const Kv4Cache &c, const int32_t *slots, int slot_heads, int n, void *k_out, void *v_out, bool bf16, hipStream_t st);
+struct Kv4Attention {
+  Kv4Cache c;
+  const void *q;
+  void *out;
+  long long ld_q, ld_out;
+  const int32_t *q_offsets, *tables, *lens;     // q_offsets null: one row a request
+  int n_req, n_rows, max_rows, max_blocks, len_heads, max_context, group;
+  float scale;
+  float *lse;
+  bool add_weight;
+};
+size_t kv4_attention_scratch_bytes(int n_req, int max_rows, int max_context, int Hq, int Hkv, int hd);
+hipError_t launch_kv4_attention(const Kv4Attention &a, bool bf16, void *scratch, hipStream_t st);
+struct Kv4Evict {
+  Kv4Cache c;
+  const int32_t *tables, *lens, *seq_lens, *budgets;
+  int n_req, max_blocks, len_heads, max_context, n_sink, n_recent;
+  int32_t *new_lens;
+};
+size_t kv4_evict_scratch_bytes(int n_req, int max_context, int Hkv);
+hipError_t launch_kv4_evict(const Kv4Evict &a, void *scratch, hipStream_t st);
