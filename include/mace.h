@@ -427,7 +427,7 @@ int mace_kv4_gather(mace_handle_t h, const mace_kv4_cache_t *cache, const int32_
  * Precision: codes and scales are exact; q is exact; probabilities are rounded to bf16 before the product with V for bf16 models and carry 24 bits for fp32 ones; all
  * sums are fp32; out is rounded once.  workspace: mace_kv4_attention_workspace_bytes for the sizes of the call (other sizes can need more or less), 256-byte aligned,
  * nothing of it read before it is written.  Outputs and workspace overlap neither an input nor each other, judged from first to last element.
- * n_req, max_rows <= 65535, n_req * max_rows <= 2^24, max_context <= 2^26. */
+ * n_req, max_rows <= 65535, max_context <= 2^26, n_req * max_rows * n_q_heads <= 2^23, n_req * n_kv_heads * (max_context + max_rows) <= 2^31. */
 size_t mace_kv4_attention_workspace_bytes(mace_handle_t h, int32_t n_req, int32_t max_rows, int32_t max_context);
 int mace_kv4_attention(mace_handle_t h, const mace_kv4_cache_t *cache, const void *q, int64_t ld_q, const int32_t *q_offsets, int32_t n_req, int32_t n_rows,
                        int32_t max_rows, const int32_t *block_tables, int32_t max_blocks_per_req, const int32_t *context_lens, int32_t len_heads,

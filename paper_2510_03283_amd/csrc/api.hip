@@ -1108,12 +1108,13 @@ int mace_kv4_gather(mace_handle_t h, const mace_kv4_cache_t *cache, const int32_
 }
 
 // Requests, rows of one request and cached tokens that the attention and the eviction take: grid limits, and token numbers that stay below 2^31.
-static bool kv4_sizes_ok(int32_t n_req, int32_t max_rows, int32_t max_context) {
-  return n_req >= 0 && n_req <= 65535 && max_rows >= 1 && max_rows <= 65535 && max_context >= 0 && max_context <= (1 << 26) && (int64_t)n_req * max_rows <= (1 << 24);
+static bool kv4_sizes_ok(mace_handle_t h, int32_t n_req, int32_t max_rows, int32_t max_context) {
+  return n_req >= 0 && n_req <= 65535 && max_rows >= 1 && max_rows <= 65535 && max_context >= 0 && max_context <= (1 << 26) &&
+         (int64_t)n_req * max_rows * h->m.n_q_heads <= (1 << 23) && (int64_t)n_req * h->m.n_kv_heads * ((int64_t)max_context + max_rows) <= (1ll << 31);
 }
 
 size_t mace_kv4_attention_workspace_bytes(mace_handle_t h, int32_t n_req, int32_t max_rows, int32_t max_context) {
-  if (!h || !kv4_sizes_ok(n_req, max_rows, max_context)) return 0;
+  if (!h || !kv4_sizes_ok(h, n_req, max_rows, max_context)) return 0;
   return align_up(std::max<size_t>(kv4_attention_scratch_bytes(n_req, max_rows, max_context, h->m.n_q_heads, h->m.n_kv_heads, h->m.head_dim), 1), 256);
 }
 
@@ -1126,7 +1127,7 @@ int mace_kv4_attention(mace_handle_t h, const mace_kv4_cache_t *cache, const voi
   const Dims D(h->m);
   Kv4Cache c;
   TRY(check_kv4(cache, D, what, &c));
-  if (!kv4_sizes_ok(n_req, max_rows, max_context) || n_rows < 0 || max_blocks_per_req < 0) return fail(MACE_BAD_SHAPE, "mace_kv4_attention: at most 65535 requests of 1..65535 rows (2^24 in all) and 2^26 cached tokens");
+  if (!kv4_sizes_ok(h, n_req, max_rows, max_context) || n_rows < 0 || max_blocks_per_req < 0) return fail(MACE_BAD_SHAPE, "mace_kv4_attention: too many requests, rows or cached tokens (at most 65535, 65535, 2^26; 2^23 rows of query heads and 2^31 tokens of kv heads in all)");
   if (n_req > 0 && n_rows > 0 && (!q || !block_tables || !context_lens || !out)) return fail(MACE_INVALID_ARG, "mace_kv4_attention: bad argument");
   if (!q_offsets && (max_rows != 1 || n_rows != n_req)) return fail(MACE_INVALID_ARG, "mace_kv4_attention: without q_offsets every request has one row");
   if (len_heads != 1 && len_heads != D.Hkv) return fail(MACE_BAD_SHAPE, "mace_kv4_attention: len_heads must be 1 or n_kv_heads");
@@ -1153,7 +1154,7 @@ int mace_kv4_attention(mace_handle_t h, const mace_kv4_cache_t *cache, const voi
 }
 
 size_t mace_kv4_evict_workspace_bytes(mace_handle_t h, int32_t n_req, int32_t max_context) {
-  if (!h || !kv4_sizes_ok(n_req, 1, max_context)) return 0;
+  if (!h || !kv4_sizes_ok(h, n_req, 1, max_context)) return 0;
   return align_up(std::max<size_t>(kv4_evict_scratch_bytes(n_req, max_context, h->m.n_kv_heads), 1), 256);
 }
 
@@ -1166,7 +1167,7 @@ int mace_kv4_evict(mace_handle_t h, const mace_kv4_cache_t *cache, const int32_t
   Kv4Cache c;
   TRY(check_kv4(cache, D, what, &c));
   if (!c.weight || !c.position) return fail(MACE_INVALID_ARG, "mace_kv4_evict: the cache needs weights and positions");
-  if (!kv4_sizes_ok(n_req, 1, max_context) || max_blocks_per_req < 0) return fail(MACE_BAD_SHAPE, "mace_kv4_evict: at most 65535 requests and 2^26 cached tokens");
+  if (!kv4_sizes_ok(h, n_req, 1, max_context) || max_blocks_per_req < 0) return fail(MACE_BAD_SHAPE, "mace_kv4_evict: too many requests or cached tokens (at most 65535 and 2^26; 2^31 tokens of kv heads in all)");
   if (n_req > 0 && (!block_tables || !context_lens || !budgets || !new_lens || (n_recent > 0 && !seq_lens))) return fail(MACE_INVALID_ARG, "mace_kv4_evict: bad argument");
   if (len_heads != 1 && len_heads != D.Hkv) return fail(MACE_BAD_SHAPE, "mace_kv4_evict: len_heads must be 1 or n_kv_heads");
   if (n_sink < 0 || n_recent < 0) return fail(MACE_INVALID_ARG, "mace_kv4_evict: n_sink and n_recent must be at least 0");

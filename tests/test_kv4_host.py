@@ -62,7 +62,7 @@ REFUSED = [
     ("gather", dict(device=1), INVALID),
     *nulls("attention", ("handle", "cache", "v", "v_scale", "q", "block_tables", "lens", "out", "work")),
     ("attention", dict(null="weight", add=1), INVALID), ("attention", dict(n_req=-1), SHAPE), ("attention", dict(n_req=65536), SHAPE), ("attention", dict(max_rows=0), SHAPE),
-    ("attention", dict(max_rows=65536), SHAPE), ("attention", dict(n_req=1000, max_rows=30000), SHAPE), ("attention", dict(max_context=-1), SHAPE),
+    ("attention", dict(max_rows=65536), SHAPE), ("attention", dict(n_req=1000, max_rows=1049), SHAPE), ("attention", dict(n_req=100, max_context=1 << 23), SHAPE), ("evict", dict(n_req=100, max_context=1 << 23), SHAPE), ("attention", dict(max_context=-1), SHAPE),
     ("attention", dict(max_context=(1 << 26) + 1), SHAPE), ("attention", dict(n_rows=-1), SHAPE), ("attention", dict(tables=-1), SHAPE), ("attention", dict(n_rows=4), INVALID),
     ("attention", dict(max_rows=2, offsets=0), INVALID), ("attention", dict(heads=2), SHAPE), ("attention", dict(scale="nan"), INVALID), ("attention", dict(scale="inf"), INVALID),
     ("attention", dict(ld_q=504), SHAPE), ("attention", dict(ld_q=516), SHAPE), ("attention", dict(ld_out=511), SHAPE), ("attention", dict(misalign="q", by=8), INVALID),
@@ -90,7 +90,7 @@ def test_refused_before_anything_is_launched(recorder, call, opts, status):
 
 GOOD = [("rotary", dict()), ("rotary", dict(n=1, n_heads=4096, hd=128)), ("rotary", dict(n=1 << 20, rot=2, inter=1)), ("append", dict()), ("append", dict(heads=4, bf16=0)),
         ("append", dict(n=1 << 22, null="position")), ("append", dict(null="weight")), ("gather", dict(hd=128)), ("gather", dict(heads=4, n=1)), ("attention", dict()),
-        ("attention", dict(n_req=65535, max_context=100)), ("attention", dict(n_req=1, max_context=1 << 26, add=1)), ("attention", dict(n_req=2, max_rows=65535, group=8)),
+        ("attention", dict(n_req=65535, max_context=100)), ("attention", dict(n_req=1, max_context=1 << 26, add=1)), ("attention", dict(n_req=2, max_rows=65535, group=8)), ("attention", dict(n_req=1000, max_rows=1048, add=1)),
         ("attention", dict(n_req=1, max_rows=33, max_context=0, hd=128, null="lse")), ("evict", dict()), ("evict", dict(n_req=65535, max_context=10)), ("evict", dict(n_req=1, max_context=1 << 26)),
         ("evict", dict(null="seq", recent=0))]
 
