@@ -484,11 +484,12 @@ def mace_rotary_frequencies(rot_dim: int, theta: float, factor: float = 1.0, ori
 
 def _head_rows(h, t, name: str, heads: int):
     """(pointer, rows, row stride) of a matrix in the handle's type whose rows begin with `heads` heads, columns adjacent."""
-    if t.dim() != 2 or t.dtype != h.io_dtype or t.get_device() != h.device or t.shape[1] < heads * h.head_dim or (t.stride(1) != 1 and t.shape[1] > 1):
+    shape, strides = t.shape, t.stride()
+    if len(shape) != 2 or t.dtype != h.io_dtype or t.get_device() != h.device or shape[1] < heads * h.head_dim or (strides[1] != 1 and shape[1] > 1):
         raise MaceError(f"{name}: a matrix of {h.io_dtype} with adjacent columns, at least {heads} heads of {h.head_dim} of them, on cuda:{h.device} is wanted, "
-                        f"got {t.dtype} {tuple(t.shape)} with strides {t.stride()} on {t.device}")
-    n = t.shape[0]
-    return t.data_ptr(), n, t.stride(0) if n > 1 else max(t.stride(0), t.shape[1])
+                        f"got {t.dtype} {tuple(shape)} with strides {strides} on {t.device}")
+    n = shape[0]
+    return t.data_ptr(), n, strides[0] if n > 1 else max(strides[0], shape[1])
 
 
 def mace_rotary(h, x, positions, inv_freq, out, n_heads: int, interleaved=False, magnitude: float = 1.0, inverse=False, stream=None):

@@ -1115,7 +1115,7 @@ static bool kv4_sizes_ok(mace_handle_t h, int32_t n_req, int32_t max_rows, int32
 
 size_t mace_kv4_attention_workspace_bytes(mace_handle_t h, int32_t n_req, int32_t max_rows, int32_t max_context) {
   if (!h || !kv4_sizes_ok(h, n_req, max_rows, max_context)) return 0;
-  return align_up(std::max<size_t>(kv4_attention_scratch_bytes(n_req, max_rows, max_context, h->m.n_q_heads, h->m.n_kv_heads, h->m.head_dim), 1), 256);
+  return align_up(std::max<size_t>(kv4_attention_scratch_bytes(n_req, max_rows, max_context, h->m.n_q_heads, h->m.n_kv_heads, h->m.head_dim, h->m.io_dtype == MACE_BF16), 1), 256);
 }
 
 int mace_kv4_attention(mace_handle_t h, const mace_kv4_cache_t *cache, const void *q, int64_t ld_q, const int32_t *q_offsets, int32_t n_req, int32_t n_rows,
@@ -1146,7 +1146,7 @@ int mace_kv4_attention(mace_handle_t h, const mace_kv4_cache_t *cache, const voi
   if (overlaps(written, read)) return fail(MACE_INVALID_ARG, "mace_kv4_attention: an output or the workspace overlaps an input or another output");
   TRY(check_device(h, what));
   const Kv4Attention a = {c, q, out, ld_q, ld_out, q_offsets, block_tables, context_lens, n_req, n_rows, max_rows, max_blocks_per_req, len_heads, max_context, D.Hq / D.Hkv,
-                          scale, lse, add_weight != 0};
+                          __builtin_ctz(D.Hq / D.Hkv), scale, lse, add_weight != 0};
   prof_mark(h, (hipStream_t)stream, T_ATTN_DECODE);
   HIP_TRY(launch_kv4_attention(a, D.bf, workspace, (hipStream_t)stream), "kv4 attention");
   prof_mark(h, (hipStream_t)stream, -1);

@@ -304,12 +304,12 @@ struct Kv4Attention {
   void *out;
   long long ld_q, ld_out;
   const int32_t *q_offsets, *tables, *lens;     // q_offsets null: one row a request
-  int n_req, n_rows, max_rows, max_blocks, len_heads, max_context, group;
+  int n_req, n_rows, max_rows, max_blocks, len_heads, max_context, group, gshift;     // group: query heads of a kv head, 1 << gshift
   float scale;
   float *lse;
   bool add_weight;
 };
-size_t kv4_attention_scratch_bytes(int n_req, int max_rows, int max_context, int Hq, int Hkv, int hd);
+size_t kv4_attention_scratch_bytes(int n_req, int max_rows, int max_context, int Hq, int Hkv, int hd, bool bf16);
 hipError_t launch_kv4_attention(const Kv4Attention &a, bool bf16, void *scratch, hipStream_t st);
 struct Kv4Evict {
   Kv4Cache c;

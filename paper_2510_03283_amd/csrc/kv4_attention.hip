@@ -28,6 +28,8 @@ constexpr float LOG2E = 1.4426950408889634f;
 struct Rows {
   int req, kvh, row0, n, ctx, m0, m1;
 };
+__device__ __forceinline__ int query_of(const Kv4Attention &a, int m) { return m >> a.gshift; }
+__device__ __forceinline__ int head_of(const Kv4Attention &a, int kvh, int m) { return (kvh << a.gshift) + (m & (a.group - 1)); }
 template <int N>
 __device__ __forceinline__ Rows rows_of(const Kv4Attention &a, int req, int kvh, int tile) {
   Rows w;
@@ -48,17 +50,18 @@ __device__ __forceinline__ Rows rows_of(const Kv4Attention &a, int req, int kvh,
   return w;
 }
 
-// Q as MFMA operand: lane (i, g) holds row i, elements g HD / 4 + 8 s .. + 7 of step s, in TERMS bf16 terms.
+// Q as MFMA operand: lane (i, g) holds row m (the last one again behind it), elements g HD / 4 + 8 s .. + 7 of step s, in TERMS bf16 terms; negated
+// where the scale is negative, so that the products' scale is not.
 template <int HD, int TERMS>
-__device__ __forceinline__ void load_q(const Kv4Attention &a, const Rows &w, int i, int g, bf16x8_t (&q)[TERMS][HD / 32]) {
-  const int m = w.m0 + i;
-  const bool ok = m < w.m1;
-  const int mc = ok ? m : w.m0;
-  const size_t o = (size_t)(w.row0 + mc / a.group) * a.ld_q + (size_t)(w.kvh * a.group + mc % a.group) * HD + g * (HD / 4);
+__device__ __forceinline__ void load_q(const Kv4Attention &a, const Rows &w, int m, int g, bf16x8_t (&q)[TERMS][HD / 32]) {
+  const int mc = min(m, w.m1 - 1);
+  const uint32_t flip = a.scale < 0.f ? 0x80008000u : 0u;
+  const size_t o = (size_t)(w.row0 + query_of(a, mc)) * a.ld_q + (size_t)head_of(a, w.kvh, mc) * HD + g * (HD / 4);
 #pragma unroll
   for (int s = 0; s < HD / 32; ++s) {
     if constexpr (TERMS == 1) {
-      q[0][s] = *(const bf16x8_t *)((const bf16_t *)a.q + o + 8 * s);
+      const uint4 u = *(const uint4 *)((const bf16_t *)a.q + o + 8 * s);
+      q[0][s] = __builtin_bit_cast(bf16x8_t, make_uint4(u.x ^ flip, u.y ^ flip, u.z ^ flip, u.w ^ flip));
     } else {
       const float4 u = *(const float4 *)((const float *)a.q + o + 8 * s), v = *((const float4 *)((const float *)a.q + o + 8 * s) + 1);
       float f[8] = {u.x, u.y, u.z, u.w, v.x, v.y, v.z, v.w};
@@ -71,11 +74,14 @@ __device__ __forceinline__ void load_q(const Kv4Attention &a, const Rows &w, int
           f[2 * e] -= __uint_as_float(r[e] << 16);
           f[2 * e + 1] -= __uint_as_float(r[e] & 0xffff0000u);
         }
-        q[t][s] = __builtin_bit_cast(bf16x8_t, make_uint4(r[0], r[1], r[2], r[3]));
+        q[t][s] = __builtin_bit_cast(bf16x8_t, make_uint4(r[0] ^ flip, r[1] ^ flip, r[2] ^ flip, r[3] ^ flip));
       }
     }
   }
 }
+
+// Scale of the products, as exponents of 2; the smallest number in place of 0, which would make -inf NaN.
+__device__ __forceinline__ float score_scale(const Kv4Attention &a) { return fmaxf(fabsf(a.scale) * LOG2E, 1.4e-45f); }
 
 // Index of a token of this request and head, and whether its block exists; else index 0, whose bytes are read and not used.
 __device__ __forceinline__ uint32_t token_of(const Kv4Cache &c, const int32_t *table, int kvh, int t, int end, bool &ok) {
@@ -91,55 +97,79 @@ typedef __attribute__((ext_vector_type(2))) uint32_t u32x2_t;
 // Codes of one lane for one S^T tile: HD / 4 elements.  (The cache is read once and should not displace what else is in the caches: 521 -> 502 us for 128
 // requests of 2048 - 8192 tokens.)
 template <int HD> struct KCodes { uint32_t w[HD / 32]; };
-template <int HD>
+template <int HD, bool ONCE = true>
 __device__ __forceinline__ KCodes<HD> load_k(const unsigned char *p) {
   KCodes<HD> r;
   if constexpr (HD == 128) {
-    const u32x4_t u = __builtin_nontemporal_load((const u32x4_t *)p);
+    const u32x4_t u = ONCE ? __builtin_nontemporal_load((const u32x4_t *)p) : *(const u32x4_t *)p;
     r.w[0] = u.x; r.w[1] = u.y; r.w[2] = u.z; r.w[3] = u.w;
   } else {
-    const u32x2_t u = __builtin_nontemporal_load((const u32x2_t *)p);
+    const u32x2_t u = ONCE ? __builtin_nontemporal_load((const u32x2_t *)p) : *(const u32x2_t *)p;
     r.w[0] = u.x; r.w[1] = u.y;
   }
   return r;
 }
 
-// What a lane holds of a turn's 64 tokens: codes and scale of token 16 j + i for S^T tile j, its 16-byte pieces of V (token by token), the scales of
-// V of tokens 16 j + 4 g .. + 3, and which of tokens 16 j + 4 g + r exist.
-template <int HD>
-struct Turn {
-  KCodes<HD> k[4];
-  uint32_t ks[4];
-  u32x4_t v[HD / 32];
-  uint32_t vs[4][HD / 32];
-  uint32_t there;                                    // bit 4 j + r
-};
-
-// Block ids of the four runs of 16 tokens of a turn (blocks of 16 tokens or more): lane l has that of run l % 4.
+// Block ids of the four runs of 16 tokens of a turn (blocks of 16 tokens or more, RUNS below): lane l has that of run l % 4.
 __device__ __forceinline__ int run_entry(const Kv4Cache &c, const int32_t *table, int t0, int end, int lane) {
   const int t = t0 + 16 * (lane & 3);
   return t < end ? table[t >> c.bshift] : -1;
 }
 
-template <int HD, bool RUNS>
-__device__ __forceinline__ void load_turn(const Kv4Cache &c, const int32_t *table, int entry, int kvh, int t0, int end, int lane, Turn<HD> &u) {
-  constexpr int NG = HD / 32, VB = HD / 2, CPT = VB / 16;
+// What a lane holds of the keys of a turn's 64 tokens: codes and scale of token 16 j + i for tile j, and where that token is: base + i (RUNS: base uniform).
+template <int HD>
+struct Keys {
+  KCodes<HD> k[4];
+  uint32_t ks[4], base[4];
+};
+// Returns which tokens exist: bit 16 j + i of the turn.
+template <int HD, bool RUNS, bool ONCE>
+__device__ __forceinline__ uint64_t load_keys(const Kv4Cache &c, const int32_t *table, int entry, int kvh, int t0, int end, int lane, Keys<HD> &u) {
+  constexpr int NG = HD / 32, KB = HD / 2;
   const int i = lane & 15, g = lane >> 4;
+  uint64_t there = 0;
   if constexpr (RUNS) {
-    uint32_t base[4];                                // uniform
-    u.there = 0;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const int blk = __builtin_amdgcn_readlane(entry, j);
       const bool ok = blk >= 0 && (uint32_t)blk < c.num_blocks;
       const uint32_t at = (((uint32_t)blk * c.Hkv + kvh) << c.bshift) + ((t0 + 16 * j) & ((1 << c.bshift) - 1));
-      base[j] = ok ? at : 0u;
-      u.there |= ok ? 15u << (4 * j) : 0u;
+      u.base[j] = ok ? at : 0u;
+      there |= ok ? (uint64_t)0xffff << (16 * j) : 0ull;
     }
 #pragma unroll
-    for (int j = 0; j < 4; ++j) u.k[j] = load_k<HD>(c.k + (size_t)base[j] * VB + (i * VB + g * (VB / 4)));
+    for (int j = 0; j < 4; ++j) u.k[j] = load_k<HD, ONCE>(c.k + (size_t)u.base[j] * KB + (i * KB + g * (KB / 4)));
 #pragma unroll
-    for (int j = 0; j < 4; ++j) u.ks[j] = (c.k_scale + (size_t)base[j] * NG)[i * NG + g * (HD / 4) / kv4::GROUP];
+    for (int j = 0; j < 4; ++j) u.ks[j] = (c.k_scale + (size_t)u.base[j] * NG)[i * NG + g * (HD / 4) / kv4::GROUP];
+  } else {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      bool ok;
+      const uint32_t tok = token_of(c, table, kvh, t0 + 16 * j + i, end, ok);
+      there |= (__ballot(ok) & 0xffff) << (16 * j);
+      u.base[j] = tok - i;
+      u.k[j] = load_k<HD, ONCE>(c.k + (size_t)tok * KB + g * (KB / 4));
+      u.ks[j] = c.k_scale[(size_t)tok * NG + g * (HD / 4) / kv4::GROUP];
+    }
+  }
+  return there;
+}
+
+// A turn of the first kernel: keys, and of the values a lane's 16-byte pieces (token by token) and the scales of tokens 16 j + 4 g .. + 3.
+template <int HD>
+struct Turn {
+  Keys<HD> keys;
+  u32x4_t v[HD / 32];
+  uint32_t vs[4][HD / 32];
+  uint64_t there;
+};
+template <int HD, bool RUNS>
+__device__ __forceinline__ void load_turn(const Kv4Cache &c, const int32_t *table, int entry, int kvh, int t0, int end, int lane, Turn<HD> &u) {
+  constexpr int NG = HD / 32, VB = HD / 2, CPT = VB / 16;
+  const int g = lane >> 4;
+  u.there = load_keys<HD, RUNS, true>(c, table, entry, kvh, t0, end, lane, u.keys);
+  if constexpr (RUNS) {
+    const uint32_t *base = u.keys.base;
 #pragma unroll
     for (int p = 0; p < CPT; ++p) {
       if constexpr (HD == 128) u.v[p] = __builtin_nontemporal_load((const u32x4_t *)(c.v + (size_t)base[p] * VB + lane * 16));
@@ -161,15 +191,6 @@ __device__ __forceinline__ void load_turn(const Kv4Cache &c, const int32_t *tabl
     }
   } else {
     bool ok;
-    u.there = 0;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const uint32_t tok = token_of(c, table, kvh, t0 + 16 * j + i, end, ok);
-      const uint64_t all = __ballot(ok);               // (tile row 4 g + r is token 4 g + r of the run)
-      u.there |= (uint32_t)((all >> (4 * g)) & 15) << (4 * j);
-      u.k[j] = load_k<HD>(c.k + (size_t)tok * VB + g * (VB / 4));
-      u.ks[j] = c.k_scale[(size_t)tok * NG + g * (HD / 4) / kv4::GROUP];
-    }
 #pragma unroll
     for (int p = 0; p < CPT; ++p) u.v[p] = *(const u32x4_t *)(c.v + (size_t)token_of(c, table, kvh, t0 + (p * 64 + lane) / CPT, end, ok) * VB + lane % CPT * 16);
 #pragma unroll
@@ -185,6 +206,40 @@ __device__ __forceinline__ void load_turn(const Kv4Cache &c, const int32_t *tabl
       else { u.vs[j][0] = w[0] | w[1] << 16; u.vs[j][1] = w[2] | w[3] << 16; }
     }
   }
+}
+// -inf in place of the products of this lane's row and tokens from `last` on (16 j + 4 g + r, counted from 4 g) or tokens that are not there.
+__device__ __forceinline__ void mask_scores(f32x4_t (&s)[4], int last, uint64_t there, int g) {
+  there >>= 4 * g;
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) s[j][r] = 16 * j + r < last && ((there >> (16 * j + r)) & 1) ? s[j][r] : -INFINITY;
+}
+// Soft-max of a row, whose tokens are spread over four lanes: probabilities are 2^(sc s - top), and `top` follows the largest product only when one is more than `lag`
+// above it.  lag = 0: the largest probability is 1, which bf16 holds exactly.  lag = MANY_LAG, where many rows make the instructions count: most turns need
+// neither an exchange between lanes nor a rescaling (16 pieces of 256 rows x 32 heads x 128 behind 4000 tokens 350 -> 319 us), and a row that one token
+// dominates has the rounding of that token's probability as well (error of such rows up to 1.4 times the output's own rounding).
+constexpr float MANY_LAG = 8.f;
+struct Softmax {
+  float top = -INFINITY, minus = 0.f, l = 0.f;        // minus: -top, 0 as long as the row has seen nothing; l: this lane's part of the sum
+};
+// Whether some row of the wave has to follow, then the factor of everything summed so far (rows that need not have 1).
+__device__ __forceinline__ bool lags(const f32x4_t (&s)[4], float sc, const Softmax &x, float lag, float &largest) {
+  largest = s[0][0];
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) largest = fmaxf(largest, s[j][r]);
+  return __any(largest * sc - x.top > lag);            // (-inf above -inf: NaN, no)
+}
+__device__ __forceinline__ float follow(float largest, float sc, Softmax &x) {
+  largest = fmaxf(largest, __shfl_xor(largest, 16, 64));
+  largest = fmaxf(largest, __shfl_xor(largest, 32, 64));
+  const float top = fmaxf(x.top, largest * sc), factor = top == x.top ? 1.f : __builtin_amdgcn_exp2f(x.top - top);
+  x.top = top;
+  x.minus = top == -INFINITY ? 0.f : -top;
+  x.l *= factor;
+  return factor;
 }
 // Scale of group gr of the token of tile j, register r.
 template <int HD>
@@ -222,8 +277,8 @@ struct States {
 __device__ __forceinline__ size_t row_id(const Kv4Attention &a, int req, int k, int head) { return ((size_t)req * a.max_rows + k) * (a.c.Hkv * a.group) + head; }
 // Splits that the tile of row k of this head had, by the tile's last row.
 __device__ __forceinline__ int splits_of(const Kv4Attention &a, const States &x, const Rows &w, int k, int head) {
-  const int m = k * a.group + head % a.group, m1 = min((m / x.tile_rows + 1) * x.tile_rows, w.n * a.group);
-  return max(1, min(x.nsplit, (w.ctx + (m1 - 1) / a.group + 1 + x.chunk - 1) / x.chunk));
+  const int m = k * a.group + (head & (a.group - 1)), m1 = min((m / x.tile_rows + 1) * x.tile_rows, w.n * a.group);
+  return max(1, min(x.nsplit, (w.ctx + query_of(a, m1 - 1) + 1 + x.chunk - 1) / x.chunk));
 }
 
 // REP: copies of each row among the 16 columns of a tile.  P is scaled for every 32 channels anew, so few rows (16 / REP) are repeated, copy c scales for groups c, c + REP, ..,
@@ -239,25 +294,25 @@ __global__ __launch_bounds__(64 * WAVES, TERMS == 1 && HD == 64 ? 4 : 2) void kv
   const int kvh = blockIdx.x / tiles, tile = blockIdx.x - kvh * tiles, split = blockIdx.y;
   const Rows w = rows_of<NR>(a, blockIdx.z, kvh, tile);
   if (w.m0 >= w.m1) return;
-  const int end = w.ctx + (w.m1 - 1) / a.group + 1;            // tokens that the last row sees
+  const int end = w.ctx + query_of(a, w.m1 - 1) + 1;            // tokens that the last row sees
   const int c0 = split * x.chunk, c1 = min(end, c0 + x.chunk);
   if (c0 >= end && split > 0) return;                          // (the first one writes the rows that see nothing)
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i = lane & 15, g = lane >> 4, copy = i / NR;
   const int32_t *table = a.tables + (size_t)w.req * a.max_blocks;
-  const int limit = w.ctx + min(w.m0 + i % NR, w.m1 - 1) / a.group + 1;  // tokens that this lane's row sees
-  const int all = w.ctx + w.m0 / a.group + 1;                  // tokens that every row sees
-  const float sc = a.scale * LOG2E;
+  const int limit = w.ctx + query_of(a, min(w.m0 + i % NR, w.m1 - 1)) + 1;  // tokens that this lane's row sees
+  const int all = w.ctx + query_of(a, w.m0) + 1;                  // tokens that every row sees
+  const float sc = score_scale(a);
 
   int t0 = c0 + wave * TURN;
   constexpr int STEP = WAVES * TURN;
   int entry = 0;
   if constexpr (RUNS) entry = run_entry(a.c, table, t0, c1, lane);
   bf16x8_t q[TERMS][NS];
-  load_q<HD, TERMS>(a, w, i % NR, g, q);
+  load_q<HD, TERMS>(a, w, w.m0 + i % NR, g, q);
   f32x4_t o[CT];
 #pragma unroll
   for (int c = 0; c < CT; ++c) o[c] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-  float m = -INFINITY, l = 0.f;
+  Softmax sx;
   unsigned char *vs = sm + wave * TURN * VROW;
   const unsigned char *vread = vs + (16 * (i >> 2) + 4 * g + (i & 3)) * VROW;          // the token whose 16 channels this lane brings to a transposing read
   unsigned char *vwrite = vs + lane / CPT * VROW + lane % CPT * 16;
@@ -273,11 +328,11 @@ __global__ __launch_bounds__(64 * WAVES, TERMS == 1 && HD == 64 ? 4 : 2) void kv
     f32x4_t s[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const float ks = kv4::scale_value(u.ks[j]);
+      const float ks = kv4::scale_value(u.keys.ks[j]);
       s[j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int st = 0; st < NS; ++st) {
-        const bf16x8_t kf = kv4::decode8(u.k[j].w[st], ks);
+        const bf16x8_t kf = kv4::decode8(u.keys.k[j].w[st], ks);
 #pragma unroll
         for (int t = TERMS - 1; t >= 0; --t) s[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, q[t][st], s[j], 0, 0, 0);
       }
@@ -288,39 +343,20 @@ __global__ __launch_bounds__(64 * WAVES, TERMS == 1 && HD == 64 ? 4 : 2) void kv
       if constexpr (RUNS) entry = run_entry(a.c, table, t0 + 2 * STEP, c1, lane);
     }
     // probabilities of tokens t0 + 16 j + 4 g + r
-    const bool whole = t0 + TURN <= min(all, c1) && __all(n.there == 0xffffu);
-    float mx = m;
+    const bool whole = t0 + TURN <= min(all, c1) && n.there == ~0ull;
+    if (!whole) mask_scores(s, min(limit, c1) - t0 - 4 * g, n.there, g);
+    float largest;
+    if (lags(s, sc, sx, 0.f, largest)) {
+      const float factor = follow(largest, sc, sx);
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) s[j][r] *= sc;
-    if (!whole) {
-      const int last = min(limit, c1) - t0 - 4 * g;
-#pragma unroll
-      for (int j = 0; j < 4; ++j)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) s[j][r] = 16 * j + r < last && ((n.there >> (4 * j + r)) & 1) ? s[j][r] : -INFINITY;
-    }
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) mx = fmaxf(mx, s[j][r]);
-    mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
-    mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-    const float base = mx == -INFINITY ? 0.f : mx;
-    if (__any(mx != m)) {                              // (a row of NaN has -inf or its last finite maximum here, and stays NaN through its sum)
-      const float alpha = __builtin_amdgcn_exp2f(m - base);      // (m = -inf: 0)
-      m = mx;
-      l *= alpha;
-#pragma unroll
-      for (int c = 0; c < CT; ++c) o[c] *= alpha;
+      for (int c = 0; c < CT; ++c) o[c] *= factor;
     }
 #pragma unroll
     for (int j = 0; j < 4; ++j)
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        s[j][r] = __builtin_amdgcn_exp2f(s[j][r] - base);
-        l += s[j][r];
+        s[j][r] = __builtin_amdgcn_exp2f(fmaf(s[j][r], sc, sx.minus));
+        sx.l += s[j][r];
       }
 #pragma unroll
     for (int pass = 0; pass < NG / REP; ++pass) {
@@ -354,16 +390,16 @@ __global__ __launch_bounds__(64 * WAVES, TERMS == 1 && HD == 64 ? 4 : 2) void kv
   }
 
   // the waves' states -> one
-  l += __shfl_xor(l, 16, 64);
-  l += __shfl_xor(l, 32, 64);
+  sx.l += __shfl_xor(sx.l, 16, 64);
+  sx.l += __shfl_xor(sx.l, 32, 64);
   __syncthreads();
   float *so = (float *)sm, *sml = so + WAVES * NR * OROW;
 #pragma unroll
   for (int c = 0; c < CT; ++c)
     if (REP == 1 || c / 2 % REP == copy) *(f32x4_t *)(so + (wave * NR + i % NR) * OROW + 16 * c + 4 * g) = o[c];
   if (lane < NR) {
-    sml[(wave * NR + i) * 2] = m;
-    sml[(wave * NR + i) * 2 + 1] = l;
+    sml[(wave * NR + i) * 2] = sx.top;
+    sml[(wave * NR + i) * 2 + 1] = sx.l;
   }
   __syncthreads();
   for (int idx = tid; idx < NR * HD; idx += 64 * WAVES) {
@@ -379,9 +415,9 @@ __global__ __launch_bounds__(64 * WAVES, TERMS == 1 && HD == 64 ? 4 : 2) void kv
       ls += sml[(k * NR + row) * 2 + 1] * f;
       as += so[(k * NR + row) * OROW + e] * f;
     }
-    const size_t r = w.row0 + mr / a.group;
-    const int head = kvh * a.group + mr % a.group, Hq = a.c.Hkv * a.group;
-    const size_t at = row_id(a, w.req, mr / a.group, head);
+    const size_t r = w.row0 + query_of(a, mr);
+    const int head = head_of(a, kvh, mr), Hq = a.c.Hkv * a.group;
+    const size_t at = row_id(a, w.req, query_of(a, mr), head);
     if (x.nsplit == 1) {
       const float v = ls == 0.f ? 0.f : as / ls;
       if constexpr (TERMS == 1) ((bf16_t *)a.out)[r * a.ld_out + (size_t)head * HD + e] = f2bf(v);
@@ -398,6 +434,210 @@ __global__ __launch_bounds__(64 * WAVES, TERMS == 1 && HD == 64 ? 4 : 2) void kv
   }
 }
 
+// Many rows of a request: a block of 128 rows, 32 a wave, goes through the tokens together.  A thread takes a group of 32 of a token's key and value: the key's codes go to LDS as they are
+// and are decoded by every wave (a quarter of the bytes that decoded ones would be read in), the value's are decoded with their scale first and lie there as bf16, token by token,
+// so that P needs no scaling and a transposing read of 4 tokens x 16 channels hands out V^T.  A value group that is NaN counts as 0 there and is noted beside it: only the
+// rows that see the token become NaN.  A turn's codes are asked for two turns ahead, put into LDS one ahead, their
+// blocks looked up three ahead.
+constexpr int ROW_TILES = 2, BLOCK_ROWS = WAVES * ROW_TILES * ROWS;
+typedef __attribute__((ext_vector_type(4))) short s16x4_t;
+typedef __attribute__((address_space(3))) s16x4_t lds_s16x4_t;
+
+template <int HD>
+__global__ __launch_bounds__(64 * WAVES, 2) void kv4_rows_kernel(Kv4Attention a, States x) {
+  constexpr int NS = HD / 32, NG = HD / 32, CT = HD / 16, VROW = HD * 2, KROW = HD / 2;
+  __shared__ __align__(16) unsigned char sv[2][TURN * VROW], sk[2][TURN * KROW], sks[2][TURN * NG];
+  __shared__ int any[3];                               // by turn, as the next two: read in it, filled in the one before, cleared in the one before that
+  __shared__ unsigned long long nan[3][NG], missing[3];
+  const int kvh = blockIdx.x % a.c.Hkv, tile = gridDim.x / a.c.Hkv - 1 - blockIdx.x / a.c.Hkv, split = blockIdx.y;      // long tiles first; the tiles of a kv head on one XCD where there are 8 heads
+  const Rows w = rows_of<BLOCK_ROWS>(a, blockIdx.z, kvh, tile);
+  if (w.m0 >= w.m1) return;
+  const int end = w.ctx + query_of(a, w.m1 - 1) + 1, c0 = split * x.chunk, c1 = min(end, c0 + x.chunk);
+  if (c0 >= end && split > 0) return;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i = lane & 15, g = lane >> 4;
+  const int32_t *table = a.tables + (size_t)w.req * a.max_blocks;
+  const float sc = score_scale(a);
+
+  // thread (token tid / NG, group tid % NG) of a turn (64-wide heads: the first 128 threads)
+  const int vt = tid / NG, vg = tid % NG;
+  const bool loads = HD == 128 || tid < TURN * NG;
+  struct Codes {
+    u32x4_t k, v;
+    uint32_t ks, vs;
+    bool ok;
+  };
+  auto entry_of = [&](int t0) { return loads && t0 + vt < c1 ? table[(t0 + vt) >> a.c.bshift] : -1; };
+  auto load = [&](int t0, int blk) {
+    Codes n;
+    n.ok = blk >= 0 && (uint32_t)blk < a.c.num_blocks;
+    const uint32_t tok = n.ok ? (((uint32_t)blk * a.c.Hkv + kvh) << a.c.bshift) + ((t0 + vt) & ((1 << a.c.bshift) - 1)) : 0u;
+    n.k = *(const u32x4_t *)(a.c.k + (size_t)tok * KROW + vg * 16);
+    n.v = *(const u32x4_t *)(a.c.v + (size_t)tok * KROW + vg * 16);
+    n.ks = a.c.k_scale[(size_t)tok * NG + vg];
+    n.vs = a.c.v_scale[(size_t)tok * NG + vg];
+    return n;
+  };
+  auto swizzle = [](int row) { return HD == 128 ? 2 * (row & 7) : 2 * ((row >> 1) & 3); };      // 16 rows' reads of one channel tile meet every bank twice
+  auto store = [&](const Codes &n, int buf, int turn) {
+    if (!loads) return;
+    *(u32x4_t *)(sk[buf] + vt * KROW + vg * 16) = n.k;
+    sks[buf][vt * NG + vg] = (unsigned char)n.ks;
+    const bool bad = n.ok && n.vs == kv4::NAN_SCALE, none = !n.ok || bad;
+    if (none) {
+      atomicOr(bad ? &nan[turn][vg] : &missing[turn], 1ull << vt);
+      any[turn] = 1;
+    }
+    const float s = none ? 1.f : kv4::scale_value(n.vs);
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      *(bf16x8_t *)(sv[buf] + vt * VROW + (((4 * vg + e) ^ swizzle(vt)) << 4)) = kv4::decode8(none ? 0u : n.v[e], s);
+  };
+
+  const int first = entry_of(c0), second = entry_of(c0 + TURN);
+  int entry = entry_of(c0 + 2 * TURN);                 // of the turn whose codes are asked for next
+  const Codes now = load(c0, first);
+  Codes codes = load(c0 + TURN, second);               // of the next turn
+  const int mw = w.m0 + wave * ROW_TILES * ROWS;
+  const int wave_end = mw < w.m1 ? w.ctx + query_of(a, min(mw + ROW_TILES * ROWS - 1, w.m1 - 1)) + 1 : 0;      // tokens that the wave's last row sees, and that all its rows see
+  const int wave_all = w.ctx + query_of(a, min(mw, w.m1 - 1)) + 1;
+  int limit[ROW_TILES];
+  bf16x8_t q[ROW_TILES][1][NS];
+  f32x4_t o[ROW_TILES][CT];
+  Softmax sx[ROW_TILES];
+#pragma unroll
+  for (int b = 0; b < ROW_TILES; ++b) {
+    const int row = mw + b * ROWS + i;
+    limit[b] = w.ctx + query_of(a, min(row, w.m1 - 1)) + 1;
+    load_q<HD, 1>(a, w, row, g, q[b]);
+#pragma unroll
+    for (int c = 0; c < CT; ++c) o[b][c] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  }
+  if (tid < 3 * NG) nan[tid / NG][tid % NG] = 0;
+  if (tid < 3) { missing[tid] = 0; any[tid] = 0; }
+  __syncthreads();
+  if (c0 < c1) store(now, 0, 0);
+  const int vrow = 4 * g + (i >> 2);
+  int buf = 0, turn = 0;
+  for (int t0 = c0; t0 < c1; t0 += TURN, buf ^= 1) {
+    __syncthreads();                                   // this turn's keys and values are there, and the other buffer is free
+    const int next = turn == 2 ? 0 : turn + 1, after = next == 2 ? 0 : next + 1;
+    if (tid < NG) nan[after][tid] = 0;
+    if (tid == 0) { missing[after] = 0; any[after] = 0; }
+    if (t0 + TURN < c1) store(codes, buf ^ 1, next);
+    if (t0 + 2 * TURN < c1) {
+      codes = load(t0 + 2 * TURN, entry);
+      entry = entry_of(t0 + 3 * TURN);
+    }
+    if (t0 < wave_end) {
+      const int marked = any[turn];
+      f32x4_t s[ROW_TILES][4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float ks = kv4::scale_value(sks[buf][(16 * j + i) * NG + g * (HD / 4) / kv4::GROUP]);
+        const KCodes<HD> k = load_k<HD, false>(sk[buf] + (16 * j + i) * KROW + g * (KROW / 4));
+#pragma unroll
+        for (int b = 0; b < ROW_TILES; ++b) s[b][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int st = 0; st < NS; ++st) {
+          const bf16x8_t kf = kv4::decode8(k.w[st], ks);
+#pragma unroll
+          for (int b = 0; b < ROW_TILES; ++b) s[b][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, q[b][0][st], s[b][j], 0, 0, 0);
+        }
+      }
+      // lane (i, g) brings channels 4 (i % 4) .. + 3 of tile c from token 16 (2 h + n) + 4 g + i / 4 and gets channel i of tokens 4 g .. + 3 of the run
+      auto read_v = [&](int c, bf16x8_t (&v)[2]) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          s16x4_t p[2];
+#pragma unroll
+          for (int n = 0; n < 2; ++n)
+            p[n] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t *)(sv[buf] + (16 * (2 * h + n) + vrow) * VROW + (((2 * c + ((i >> 1) & 1)) ^ swizzle(vrow)) << 4) + 8 * (i & 1)));
+          v[h] = __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(p[0], p[1], 0, 1, 2, 3, 4, 5, 6, 7));
+        }
+      };
+      bf16x8_t vf[2];
+      read_v(0, vf);
+      const bool whole = t0 + TURN <= min(wave_all, c1) && !marked;
+      const uint64_t there = marked ? ~missing[turn] : ~0ull;
+      bf16x8_t pf[ROW_TILES][2][1];
+#pragma unroll
+      for (int b = 0; b < ROW_TILES; ++b) {
+        if (!whole) mask_scores(s[b], min(limit[b], c1) - t0 - 4 * g, there, g);
+        float largest;
+        if (lags(s[b], sc, sx[b], MANY_LAG, largest)) {
+          const float factor = follow(largest, sc, sx[b]);
+#pragma unroll
+          for (int c = 0; c < CT; ++c) o[b][c] *= factor;
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          float f[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            f[e] = __builtin_amdgcn_exp2f(fmaf(s[b][2 * h + (e >> 2)][e & 3], sc, sx[b].minus));
+            sx[b].l += f[e];
+          }
+          split8<1>(f, pf[b][h]);
+        }
+      }
+      // operands of the next channel tile are read before the products of this one (left to itself, the compiler reads each where it is used and waits)
+#pragma unroll
+      for (int c = 0; c < CT; ++c) {
+        bf16x8_t vn[2];
+        if (c + 1 < CT) read_v(c + 1, vn);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int b = 0; b < ROW_TILES; ++b) o[b][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[h], pf[b][h][0], o[b][c], 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);
+        vf[0] = vn[0];
+        vf[1] = vn[1];
+      }
+      if (marked) {
+#pragma unroll
+        for (int gr = 0; gr < NG; ++gr) {
+          const uint64_t bad = nan[turn][gr];
+#pragma unroll
+          for (int b = 0; b < ROW_TILES; ++b) {
+            const int last = limit[b] - t0;            // the row sees tokens below it
+            const uint64_t seen = last >= 64 ? bad : last > 0 ? bad & ((1ull << last) - 1) : 0ull;
+            if (seen) { o[b][2 * gr] = f32x4_t{NAN, NAN, NAN, NAN}; o[b][2 * gr + 1] = o[b][2 * gr]; }
+          }
+        }
+      }
+    }
+    turn = next;
+  }
+
+#pragma unroll
+  for (int b = 0; b < ROW_TILES; ++b) {
+    float l = sx[b].l;
+    l += __shfl_xor(l, 16, 64);
+    l += __shfl_xor(l, 32, 64);
+    const int mr = mw + b * ROWS + i;
+    if (mr >= w.m1) continue;
+    const int k = query_of(a, mr), head = head_of(a, kvh, mr), Hq = a.c.Hkv * a.group;
+    const size_t r = w.row0 + k, at = row_id(a, w.req, k, head);
+    if (x.nsplit == 1) {
+      const float inv = l == 0.f ? 0.f : 1.f / l;
+      bf16_t *to = (bf16_t *)a.out + r * a.ld_out + (size_t)head * HD + 4 * g;
+#pragma unroll
+      for (int c = 0; c < CT; ++c) *(uint2 *)(to + 16 * c) = make_uint2(cvt_pk_bf16(o[b][c][0] * inv, o[b][c][1] * inv), cvt_pk_bf16(o[b][c][2] * inv, o[b][c][3] * inv));
+      if (g == 0) {
+        const float lse2 = l == 0.f ? -INFINITY : sx[b].top + log2f(l);
+        if (a.lse) a.lse[r * Hq + head] = lse2 / LOG2E;
+        if (a.add_weight) x.lse2[at] = lse2;
+      }
+    } else {
+      float *to = x.acc + (at * x.nsplit + split) * HD + 4 * g;
+#pragma unroll
+      for (int c = 0; c < CT; ++c) *(f32x4_t *)(to + 16 * c) = o[b][c];
+      if (g == 0) x.ml[at * x.nsplit + split] = make_float2(sx[b].top, l);
+    }
+  }
+}
+
 // Joins the splits of a row and head: `groups` teams of HD / 4 lanes (four channels each) take every groups-th split with a soft-max state of their own and are merged
 // in order.  The time is the latency of the loads, so a team has those of IN_FLIGHT splits under way.
 constexpr int IN_FLIGHT = 4;
@@ -407,7 +647,7 @@ __device__ __forceinline__ void join_rows(const Kv4Attention &a, const States &x
   const int Hq = a.c.Hkv * a.group, team = threadIdx.x / LANES, e = threadIdx.x % LANES, grp = team % groups;
   const size_t at = (size_t)block * (64 * WAVES / LANES / groups) + team / groups, rows = (size_t)a.n_req * a.max_rows * Hq;
   const int head = (int)(at % Hq), k = (int)(at / Hq % a.max_rows), req = (int)(min(at, rows - 1) / Hq / a.max_rows);
-  const Rows w = rows_of<1>(a, req, head / a.group, 0);
+  const Rows w = rows_of<1>(a, req, head >> a.gshift, 0);
   const bool live = at < rows && k < w.n;
   const int ns = live ? splits_of(a, x, w, k, head) : 0;
   const float *acc = x.acc + at * x.nsplit * HD;
@@ -497,37 +737,16 @@ __global__ __launch_bounds__(64 * WAVES) void kv4_weight_kernel(Kv4Attention a, 
   if (w.n == 0 || piece * WAVES * TURN >= end) return;
   const int t0 = (piece * WAVES + wave) * TURN;
   const int32_t *table = a.tables + (size_t)req * a.max_blocks;
-  const float sc = a.scale * LOG2E;
-  // keys
-  KCodes<HD> k[4];
-  uint32_t ks[4], tok[4], there = 0;
-  if constexpr (RUNS) {
-    const int entry = run_entry(a.c, table, t0, end, lane);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int blk = __builtin_amdgcn_readlane(entry, j);
-      const bool ok = blk >= 0 && (uint32_t)blk < a.c.num_blocks;
-      const uint32_t at = (((uint32_t)blk * a.c.Hkv + kvh) << a.c.bshift) + ((t0 + 16 * j) & ((1 << a.c.bshift) - 1)), base = ok ? at : 0u;
-      there |= ok ? 1u << j : 0u;
-      tok[j] = base + i;
-      k[j] = load_k<HD>(a.c.k + (size_t)base * (HD / 2) + (i * (HD / 2) + g * (HD / 8)));
-      ks[j] = (a.c.k_scale + (size_t)base * (HD / 32))[i * (HD / 32) + g * (HD / 4) / kv4::GROUP];
-    }
-  } else {
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      bool ok;
-      tok[j] = token_of(a.c, table, kvh, t0 + 16 * j + i, end, ok);
-      there |= ok ? 1u << j : 0u;
-      k[j] = load_k<HD>(a.c.k + (size_t)tok[j] * (HD / 2) + g * (HD / 8));
-      ks[j] = a.c.k_scale[(size_t)tok[j] * (HD / 32) + g * (HD / 4) / kv4::GROUP];
-    }
-  }
+  const float sc = score_scale(a);
+  Keys<HD> u;
+  int entry = 0;
+  if constexpr (RUNS) entry = run_entry(a.c, table, t0, end, lane);
+  const uint64_t there = load_keys<HD, RUNS, false>(a.c, table, entry, kvh, t0, end, lane, u);
   bf16x8_t q[TERMS][NS];
-  load_q<HD, TERMS>(a, w, i, g, q);
+  load_q<HD, TERMS>(a, w, w.m0 + i, g, q);
   // log sums of the rows: 16 threads a row
   {
-    const int row = threadIdx.x / 16, mr = min(row, w.m1 - 1), kr = mr / a.group, head = kvh * a.group + mr % a.group;
+    const int row = threadIdx.x / 16, mr = min(row, w.m1 - 1), kr = query_of(a, mr), head = head_of(a, kvh, mr);
     const float2 *ml = x.ml + row_id(a, req, kr, head) * x.nsplit;
     const int ns = splits_of(a, x, w, kr, head);
     float mn = -INFINITY, ls = 0.f;
@@ -552,15 +771,15 @@ __global__ __launch_bounds__(64 * WAVES) void kv4_weight_kernel(Kv4Attention a, 
   for (int r = 0; r < 4; ++r) {
     const int m = 4 * g + r;
     lse2[r] = slse[m];
-    last[r] = m < w.m1 ? w.ctx + m / a.group + 1 : 0;
+    last[r] = m < w.m1 ? w.ctx + query_of(a, m) + 1 : 0;
   }
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
-    const float scale = kv4::scale_value(ks[j]);
+    const float scale = kv4::scale_value(u.ks[j]);
     f32x4_t s = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int st = 0; st < NS; ++st) {
-      const bf16x8_t kf = kv4::decode8(k[j].w[st], scale);
+      const bf16x8_t kf = kv4::decode8(u.k[j].w[st], scale);
 #pragma unroll
       for (int t = TERMS - 1; t >= 0; --t) s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(q[t][st], kf, s, 0, 0, 0);
     }
@@ -569,20 +788,68 @@ __global__ __launch_bounds__(64 * WAVES) void kv4_weight_kernel(Kv4Attention a, 
     for (int r = 0; r < 4; ++r) sum += t0 + 16 * j + i < last[r] ? __builtin_amdgcn_exp2f(s[r] * sc - lse2[r]) : 0.f;
     sum += __shfl_xor(sum, 16, 64);
     sum += __shfl_xor(sum, 32, 64);
-    if (g == j && ((there >> j) & 1) && t0 + 16 * j + i < end) unsafeAtomicAdd(a.c.weight + tok[j], sum);
+    if (g == j && ((there >> (16 * j + i)) & 1) && t0 + 16 * j + i < end) unsafeAtomicAdd(a.c.weight + (u.base[j] + i), sum);
   }
 }
 
-// The same for more rows, whose log sums are there already.
+// The same for more rows, whose log sums are there already.  A wave keeps the decoded keys of its 64 tokens; the rows come in stages of 64 (fp32: 16) through LDS,
+// shared by the waves of a block, a stage ahead in registers.
 template <int HD, int TERMS>
-__global__ __launch_bounds__(64 * WAVES) void kv4_weight_rows_kernel(Kv4Attention a, States x) {
-  constexpr int NS = HD / 32, NG = HD / 32;
-  const int kvh = blockIdx.y, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = lane & 15, g = lane >> 4;
-  Rows w = rows_of<ROWS>(a, blockIdx.z, kvh, 0);
-  const int end = w.ctx + w.n, t0 = (blockIdx.x * WAVES + wave) * TURN;
-  if (w.n == 0 || t0 >= end) return;
+__global__ __launch_bounds__(64 * WAVES, 2) void kv4_weight_rows_kernel(Kv4Attention a, States x) {
+  constexpr int NS = HD / 32, NG = HD / 32, STAGE = TERMS == 1 ? 64 : 16, CPR = HD / 8;      // 16-byte pieces of a row in bf16
+  constexpr int PER = STAGE * CPR / (64 * WAVES) ? STAGE * CPR / (64 * WAVES) : 1;            // pieces a thread brings
+  __shared__ __align__(16) uint4 sq[2][TERMS][STAGE * CPR];
+  __shared__ __align__(16) float slse[2][STAGE];
+  const int kvh = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, i = lane & 15, g = lane >> 4;
+  const Rows w = rows_of<1>(a, blockIdx.z, kvh, 0);
+  const int n_rows = w.n * a.group, end = w.ctx + w.n, b0 = blockIdx.x * WAVES * TURN, t0 = b0 + wave * TURN;
+  if (n_rows == 0 || b0 >= end) return;
   const int32_t *table = a.tables + (size_t)w.req * a.max_blocks;
-  const float sc = a.scale * LOG2E;
+  const float sc = score_scale(a);
+  auto swizzle = [](int row) { return HD == 128 ? row & 15 : (row >> 1) & 7; };      // the 16 rows of a read lie in different banks
+  // pieces of the rows from m0 on: thread -> (row, piece); behind the last row the last one again, with a log sum that leaves nothing of it
+  uint4 piece[TERMS][PER];
+  float lse2 = INFINITY;
+  auto load = [&](int m0) {
+#pragma unroll
+    for (int p = 0; p < PER; ++p) {
+      const int at = p * 64 * WAVES + tid, m = min(m0 + at / CPR, n_rows - 1);
+      if (at >= STAGE * CPR) continue;
+      const size_t o = (size_t)(w.row0 + query_of(a, m)) * a.ld_q + (size_t)head_of(a, kvh, m) * HD + at % CPR * 8;
+      if constexpr (TERMS == 1) {
+        piece[0][p] = *(const uint4 *)((const bf16_t *)a.q + o);
+      } else {
+        const float4 u = *(const float4 *)((const float *)a.q + o), v = *((const float4 *)((const float *)a.q + o) + 1);
+        float f[8] = {u.x, u.y, u.z, u.w, v.x, v.y, v.z, v.w};
+        bf16x8_t y[TERMS];
+        split8<TERMS>(f, y);
+#pragma unroll
+        for (int t = 0; t < TERMS; ++t) piece[t][p] = __builtin_bit_cast(uint4, y[t]);
+      }
+    }
+    if (tid < STAGE) {
+      const int m = m0 + tid, mc = min(m, n_rows - 1);
+      lse2 = x.lse2[row_id(a, w.req, query_of(a, mc), head_of(a, kvh, mc))];
+      if (m >= n_rows || lse2 == -INFINITY) lse2 = INFINITY;
+    }
+  };
+  const uint32_t flip = a.scale < 0.f ? 0x80008000u : 0u;
+  auto store = [&](int buf) {
+#pragma unroll
+    for (int p = 0; p < PER; ++p) {
+      const int at = p * 64 * WAVES + tid;
+      if (at >= STAGE * CPR) continue;
+#pragma unroll
+      for (int t = 0; t < TERMS; ++t) {
+        const uint4 u = piece[t][p];
+        sq[buf][t][at / CPR * CPR + (at % CPR ^ swizzle(at / CPR))] = make_uint4(u.x ^ flip, u.y ^ flip, u.z ^ flip, u.w ^ flip);
+      }
+    }
+    if (tid < STAGE) slse[buf][tid] = lse2;
+  };
+
+  const int first = max(0, b0 - w.ctx) * a.group / ROWS * ROWS;      // rows before it see none of the block's tokens
+  load(first);
   bf16x8_t kf[4][NS];
   uint32_t tok[4];
   bool ok[4];
@@ -590,34 +857,48 @@ __global__ __launch_bounds__(64 * WAVES) void kv4_weight_rows_kernel(Kv4Attentio
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     tok[j] = token_of(a.c, table, kvh, t0 + 16 * j + i, end, ok[j]);
-    const KCodes<HD> k = load_k<HD>(a.c.k + (size_t)tok[j] * (HD / 2) + g * (HD / 8));
+    const KCodes<HD> k = load_k<HD, false>(a.c.k + (size_t)tok[j] * (HD / 2) + g * (HD / 8));
     const float ks = kv4::scale_value(a.c.k_scale[(size_t)tok[j] * NG + g * (HD / 4) / kv4::GROUP]);
 #pragma unroll
     for (int st = 0; st < NS; ++st) kf[j][st] = kv4::decode8(k.w[st], ks);
   }
-  const int first = max(0, t0 - w.ctx);              // queries before it see none of these tokens
-  for (w.m0 = first * a.group / ROWS * ROWS; w.m0 < w.n * a.group; w.m0 += ROWS) {
-    w.m1 = min(w.m0 + ROWS, w.n * a.group);
-    bf16x8_t q[TERMS][NS];
-    load_q<HD, TERMS>(a, w, i, g, q);
-    float lse2[4];
-    int last[4];
+  store(0);
+  int buf = 0;
+  for (int m0 = first; m0 < n_rows; m0 += STAGE, buf ^= 1) {
+    __syncthreads();
+    if (m0 + STAGE < n_rows) load(m0 + STAGE);
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      const int m = w.m0 + 4 * g + r, mc = min(m, w.m1 - 1);
-      lse2[r] = x.lse2[row_id(a, w.req, mc / a.group, kvh * a.group + mc % a.group)];
-      last[r] = m < w.m1 ? w.ctx + mc / a.group + 1 : 0;
+    for (int r0 = 0; r0 < STAGE; r0 += ROWS) {         // (behind the last row: nothing is added)
+      bf16x8_t q[TERMS][NS];
+#pragma unroll
+      for (int t = 0; t < TERMS; ++t)
+#pragma unroll
+        for (int st = 0; st < NS; ++st) q[t][st] = __builtin_bit_cast(bf16x8_t, sq[buf][t][(r0 + i) * CPR + ((g * (CPR / 4) + st) ^ swizzle(i))]);
+      const f32x4_t ls = *(const f32x4_t *)(slse[buf] + r0 + 4 * g);
+      const bool whole = t0 + TURN <= w.ctx + query_of(a, m0 + r0) + 1;
+      f32x4_t s[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        s[j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int st = 0; st < NS; ++st)
+#pragma unroll
+          for (int t = TERMS - 1; t >= 0; --t) s[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(q[t][st], kf[j][st], s[j], 0, 0, 0);
+      }
+      if (!whole) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int last = w.ctx + query_of(a, m0 + r0 + 4 * g + r) + 1 - t0 - i;      // the row sees tokens below it
+#pragma unroll
+          for (int j = 0; j < 4; ++j) s[j][r] = 16 * j < last ? s[j][r] : -INFINITY;
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) sum[j] += __builtin_amdgcn_exp2f(fmaf(s[j][r], sc, -ls[r]));
     }
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      f32x4_t s = f32x4_t{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int st = 0; st < NS; ++st)
-#pragma unroll
-        for (int t = TERMS - 1; t >= 0; --t) s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(q[t][st], kf[j][st], s, 0, 0, 0);
-#pragma unroll
-      for (int r = 0; r < 4; ++r) sum[j] += ok[j] && t0 + 16 * j + i < last[r] ? __builtin_amdgcn_exp2f(s[r] * sc - lse2[r]) : 0.f;
-    }
+    if (m0 + STAGE < n_rows) store(buf ^ 1);
   }
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
@@ -627,23 +908,43 @@ __global__ __launch_bounds__(64 * WAVES) void kv4_weight_rows_kernel(Kv4Attentio
   }
 }
 
-// Tokens of a block: enough blocks to fill the chip, not below a turn of all its waves.
+// Tokens of a block: 4096, less where that makes fewer blocks than two a CU, not below four turns of its waves (a second launch to join splits costs
+// more than it saves below that).  us at 256 / 512 / 1024 / 2048 / 4096 tokens, one row a request, 4 query heads a kv head: 4 requests of 400 - 1000 tokens, 8 kv heads of 128
+// 15.4 / 12.5 / 11.2 / 12.0 / 11.1; 16 of 1500 - 4000 22.5 / 22.1 / 19.9 / 22.3 / 26.9; 64 of 1500 - 4000 61 / 55 / 52 / 52 / 43; 1 of 60000 29.2 / 23.8 / 22.7 / 23.7 / 31.6;
+// 256 of 8000 - 16000 863 / 751 / 686 / 654 / 627.
 int chunk_tokens(int n_req, int tiles, int Hkv, int tokens) {
   int chunk = 4096;
-  while (chunk > 256 && (long long)n_req * Hkv * tiles * cdiv(tokens, chunk) < 1024) chunk /= 2;
+  while (chunk > 4 * WAVES * TURN && (long long)n_req * Hkv * tiles * cdiv(tokens, chunk) < 512) chunk /= 2;
   return chunk;
+}
+// Rows of a kv head up to which the first kernel takes bf16 requests, tile by tile; us on it and on the kernel of many rows, 64 requests of 2000 tokens, 8 kv heads: 16 / 24 / 32 rows
+// of 128-wide heads 45 and 62 / 66 and 63 / 67 and 63, 32 / 48 / 64 rows of 64-wide ones 40 and 49 / 56 and 62 / 73 and 63.
+int few_rows(int hd) { return hd == 128 ? 16 : 48; }
+// Two blocks a CU, or splits of four turns.
+int rows_chunk(int n_req, int tiles, int Hkv, int tokens) {
+  const long long blocks = (long long)n_req * Hkv * tiles;
+  const int nsplit = (int)std::max(1ll, std::min<long long>(cdiv(tokens, 4 * TURN), (512 + blocks - 1) / blocks));
+  return cdiv(cdiv(tokens, nsplit), TURN) * TURN;
 }
 // Copies of a row in a tile: as many as rows and scale groups leave room for.
 int copies(int rows, int hd) { return rows <= 4 && hd == 128 ? 4 : rows <= 8 ? 2 : 1; }
 
 struct Plan {
-  int rep, tiles, nsplit, chunk;
+  bool many;                 // blocks of many rows
+  int rep, tile_rows, tiles, nsplit, chunk;
   size_t rows;
 };
-Plan plan_of(int n_req, int max_rows, int max_context, int Hq, int Hkv, int hd) {
-  const int rows = max_rows * (Hq / Hkv), tokens = max_context + max_rows, rep = copies(rows, hd), tiles = cdiv(rows, ROWS / rep);
-  const int chunk = chunk_tokens(n_req, tiles, Hkv, tokens);
-  return {rep, tiles, cdiv(tokens, chunk), chunk, (size_t)n_req * max_rows * Hq};
+Plan plan_of(int n_req, int max_rows, int max_context, int Hq, int Hkv, int hd, bool bf16) {
+  Plan p;
+  const int rows = max_rows * (Hq / Hkv), tokens = max_context + max_rows;
+  p.many = bf16 && rows > few_rows(hd);
+  p.rep = copies(rows, hd);
+  p.tile_rows = p.many ? BLOCK_ROWS : ROWS / p.rep;
+  p.tiles = cdiv(rows, p.tile_rows);
+  p.chunk = p.many ? rows_chunk(n_req, p.tiles, Hkv, tokens) : chunk_tokens(n_req, p.tiles, Hkv, tokens);
+  p.nsplit = cdiv(tokens, p.chunk);
+  p.rows = (size_t)n_req * max_rows * Hq;
+  return p;
 }
 // (acc is there for several splits only)
 size_t ml_bytes(const Plan &p) { return align_up(p.rows * p.nsplit * sizeof(float2), 256); }
@@ -651,19 +952,20 @@ size_t lse_bytes(const Plan &p) { return align_up(p.rows * sizeof(float), 256); 
 
 }  // namespace
 
-size_t kv4_attention_scratch_bytes(int n_req, int max_rows, int max_context, int Hq, int Hkv, int hd) {
-  const Plan p = plan_of(n_req, max_rows, max_context, Hq, Hkv, hd);
+size_t kv4_attention_scratch_bytes(int n_req, int max_rows, int max_context, int Hq, int Hkv, int hd, bool bf16) {
+  const Plan p = plan_of(n_req, max_rows, max_context, Hq, Hkv, hd, bf16);
   return ml_bytes(p) + lse_bytes(p) + (p.nsplit > 1 ? p.rows * p.nsplit * hd * sizeof(float) : 0);
 }
 
 hipError_t launch_kv4_attention(const Kv4Attention &a, bool bf16, void *scratch, hipStream_t st) {
   if (a.n_req <= 0 || a.n_rows <= 0) return hipSuccess;
   const int Hkv = a.c.Hkv, hd = a.c.hd, tokens = a.max_context + a.max_rows;
-  const Plan p = plan_of(a.n_req, a.max_rows, a.max_context, Hkv * a.group, Hkv, hd);
+  const Plan p = plan_of(a.n_req, a.max_rows, a.max_context, Hkv * a.group, Hkv, hd, bf16);
   const bool runs = a.c.bshift >= 4;
   char *at = (char *)scratch;
-  const States x = {(float *)(at + ml_bytes(p) + lse_bytes(p)), (float2 *)at, (float *)(at + ml_bytes(p)), p.nsplit, p.chunk, ROWS / p.rep};
+  const States x = {(float *)(at + ml_bytes(p) + lse_bytes(p)), (float2 *)at, (float *)(at + ml_bytes(p)), p.nsplit, p.chunk, p.tile_rows};
   auto main = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(Hkv * p.tiles, p.nsplit, a.n_req), dim3(64 * WAVES), 0, st, a, x, p.tiles); };
+  auto many = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(Hkv * p.tiles, p.nsplit, a.n_req), dim3(64 * WAVES), 0, st, a, x); };
   // teams of a row and head: one up to the splits that it has under way at once, else four or all of a block
   const int teams = 64 * WAVES / (hd / 4), groups = p.nsplit <= IN_FLIGHT ? 1 : p.nsplit <= 4 * IN_FLIGHT ? 4 : teams;
   const int joins = p.nsplit > 1 ? (int)((p.rows * groups + teams - 1) / teams) : 0, pieces = cdiv(tokens, TURN * WAVES);
@@ -674,7 +976,11 @@ hipError_t launch_kv4_attention(const Kv4Attention &a, bool bf16, void *scratch,
   auto pick = [&](auto terms, auto in_runs) {
     constexpr int T = decltype(terms)::value;
     constexpr bool R = decltype(in_runs)::value;
-    if (hd == 128) p.rep == 4 ? main(kv4_attention_kernel<128, T, 4, R>) : p.rep == 2 ? main(kv4_attention_kernel<128, T, 2, R>) : main(kv4_attention_kernel<128, T, 1, R>);
+    if constexpr (T == 1) {
+      if (p.many) hd == 128 ? many(kv4_rows_kernel<128>) : many(kv4_rows_kernel<64>);
+    }
+    if (p.many) {}
+    else if (hd == 128) p.rep == 4 ? main(kv4_attention_kernel<128, T, 4, R>) : p.rep == 2 ? main(kv4_attention_kernel<128, T, 2, R>) : main(kv4_attention_kernel<128, T, 1, R>);
     else p.rep == 2 ? main(kv4_attention_kernel<64, T, 2, R>) : main(kv4_attention_kernel<64, T, 1, R>);
     if (a.add_weight && one_tile) hd == 128 ? weight(kv4_weight_kernel<128, T, R>) : weight(kv4_weight_kernel<64, T, R>);
     else if (joins) hd == 128 ? join(kv4_join_kernel<128, T == 1>) : join(kv4_join_kernel<64, T == 1>);

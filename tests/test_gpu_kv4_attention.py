@@ -91,7 +91,8 @@ def test_one_row_a_request(torch_mod, bf16, hkv, group, hd, size, lens):
 @pytest.mark.parametrize("bf16", [True, False])
 @pytest.mark.parametrize("hkv,group,hd,size,lens,counts,gap", [
     (2, 1, 64, 16, [0, 5, 40], [1, 17, 3], 0), (1, 4, 128, 16, [100, 0, 250], [5, 33, 1], 2), (2, 8, 64, 16, [63, 64, 65], [2, 2, 2], 0), (1, 1, 128, 16, [0], [150], 1),
-    (1, 2, 64, 8, [300, 20, 7, 1], [0, 40, 0, 9], 0), (1, 8, 128, 64, [600], [37], 3), (1, 1, 64, 16, [1500, 3], [1, 70], 0)])
+    (1, 2, 64, 8, [300, 20, 7, 1], [0, 40, 0, 9], 0), (1, 8, 128, 64, [600], [37], 3), (1, 1, 64, 16, [1500, 3], [1, 70], 0),
+    (1, 1, 128, 16, [2100, 5], [130, 3], 0), (2, 2, 64, 4, [1100], [65], 0), (1, 4, 64, 32, [0, 1, 62], [64, 32, 90], 0)])
 def test_several_rows_a_request(torch_mod, bf16, hkv, group, hd, size, lens, counts, gap):
     run(torch_mod, bf16, hkv, group, hd, size, lens, counts, gap=gap, seed=sum(lens) + sum(counts))
 
@@ -152,45 +153,46 @@ def test_missing_blocks_and_rows_without_a_token(torch_mod, bf16):
         assert (out3[:8] == 0).all() and torch.isneginf(lse3[:8]).all() and torch.isfinite(lse3[8:]).all()
 
 
-def test_nan_stays_where_it_is_attended_to(torch_mod):
+@pytest.mark.parametrize("hd,count", [(128, 6), (128, 40), (64, 70)])
+def test_nan_stays_where_it_is_attended_to(torch_mod, hd, count):
     """A NaN key makes NaN the rows that see it, a NaN value their 32 columns, a NaN query its own row; the other rows keep their bits."""
     torch = torch_mod
-    hkv, group, hd, size = 2, 2, 128, 16
+    hkv, group, size = 2, 2, 16
     with Model(hkv, hd, True, group) as (B, h):
         cache = R.Cache(B, 30, hkv, size, hd, 9)
-        tables = np.stack([cache.request(90, 8), cache.request(70, 8)])
+        tables = np.stack([cache.request(80 + count, 10), cache.request(70, 10)])
         s = cache.upload(B)
-        q = torch.randn((10, 4 * hd), generator=torch.Generator().manual_seed(1)).to(torch.bfloat16).cuda()
-        off = torch.tensor([0, 6, 10], dtype=torch.int32, device="cuda")
+        n, see = count + 4, 3                                           # rows 3 .. count - 1 of request 0 see token 83
+        q = torch.randn((n, 4 * hd), generator=torch.Generator().manual_seed(1)).to(torch.bfloat16).cuda()
+        off = torch.tensor([0, count, n], dtype=torch.int32, device="cuda")
         lens = torch.tensor([80, 60], dtype=torch.int32, device="cuda")
 
         def go():
             out = torch.empty_like(q)
-            B.mace_kv4_attention(h, s, q, torch.from_numpy(tables).cuda(), lens, out, workspace(torch, B, h, 2, 6, 80), 80, q_offsets=off, max_rows=6)
+            B.mace_kv4_attention(h, s, q, torch.from_numpy(tables).cuda(), lens, out, workspace(torch, B, h, 2, count, 80), 80, q_offsets=off, max_rows=count)
             torch.cuda.synchronize()
-            return out.view(10, 4, hd)
+            return out.view(n, 4, hd)
 
         clean = go()
-        at = (int(tables[0, 83 // 16]), 1, 83 % 16)                    # token 83 of request 0, head 1: rows 3 .. 5 see it
-        codes = cache.dev["v"][at][32:48].clone()
-        cache.dev["v_scale"][at][2], cache.dev["v"][at][32:48] = 255, 0       # as the append leaves it
+        at = (int(tables[0, 83 // 16]), 1, 83 % 16)
+        codes, old = cache.dev["v"][at][16:32].clone(), int(cache.dev["v_scale"][at][1])
+        cache.dev["v_scale"][at][1], cache.dev["v"][at][16:32] = 255, 0       # as the append leaves it
         got = go()
-        assert torch.isnan(got[3:6, 2:, 64:96]).all()
-        got[3:6, 2:, 64:96] = clean[3:6, 2:, 64:96]
+        assert torch.isnan(got[see:count, 2:, 32:64]).all()
+        got[see:count, 2:, 32:64] = clean[see:count, 2:, 32:64]
         assert torch.equal(got, clean)
-        cache.dev["v_scale"][at][2], cache.dev["v"][at][32:48] = 125, codes
-        clean = go()
+        cache.dev["v_scale"][at][1], cache.dev["v"][at][16:32] = old, codes
+        old = int(cache.dev["k_scale"][at][0])
         cache.dev["k_scale"][at][0] = 255
         got = go()
-        assert torch.isnan(got[3:6, 2:]).all()
-        got[3:6, 2:] = clean[3:6, 2:]
-        cache.dev["k_scale"][at][0] = 125
-        assert torch.equal(got[:3], clean[:3]) and torch.equal(got[6:], clean[6:]) and torch.equal(got[:, :2], clean[:, :2])
-        clean = go()
-        q[7, :hd] = float("nan")
+        assert torch.isnan(got[see:count, 2:]).all()
+        got[see:count, 2:] = clean[see:count, 2:]
+        assert torch.equal(got, clean)
+        cache.dev["k_scale"][at][0] = old
+        q[count + 1, :hd] = float("nan")
         got = go()
-        assert torch.isnan(got[7, 0]).all()
-        got[7, 0] = clean[7, 0]
+        assert torch.isnan(got[count + 1, 0]).all()
+        got[count + 1, 0] = clean[count + 1, 0]
         assert torch.equal(got, clean)
 
 
