@@ -16,7 +16,7 @@ struct Vec {
   struct alignas(V * sizeof(elem)) type { elem e[V]; };
 };
 
-// The quotient by a number below 2^16 that the host gives as ceil(2^32 / d); exact as long as x * d is below 2^32.
+// The quotient of x below n by d, which the host gives as ceil(2^32 / d): exact, because n * d is at most 2^32.  0 where n is no more than d.
 struct Divisor {
   uint32_t d, mul;
 };
@@ -72,18 +72,19 @@ __global__ __launch_bounds__(THREADS) void rotary_kernel(Rotary a, int rows, Div
   }
 }
 
-Divisor divisor(int d) { return {(uint32_t)d, (uint32_t)(((1ull << 32) + d - 1) / d)}; }
+Divisor divisor(int64_t n, int d) { return {(uint32_t)d, n <= d ? 0 : (uint32_t)(((1ull << 32) + d - 1) / d)}; }
 
 // Rows of a block: as many as a quarter of its threads form the angles of at once and as give each thread two items, as long as there are 1024 blocks, and within 16 KB of
 // angles.  (66576 rows of 64 heads of 128, 64 columns turned: at four times as many 449 us, now 402, 5.4 TB/s; 12289 x 40 x 128 in fp32 100 and 92.)
 template <bool BF16, int V>
 void launch(const Rotary &a, hipStream_t st) {
   const int half = a.rot / 2, copied = a.x == a.out ? 0 : (a.hd - a.rot) / (2 * V), head_items = half / V + copied, items = a.n_heads * head_items;
-  const int rows = std::max(1, std::min({std::max(THREADS / half / 4, cdiv(2 * THREADS, items)), a.n / 1024, 2048 / half}));
+  const int exact = (int)std::min((1ll << 32) / ((long long)items * items), 2048ll);           // rows that `divisor` holds for
+  const int rows = std::max(1, std::min({std::max(THREADS / half / 4, cdiv(2 * THREADS, items)), a.n / 1024, 2048 / half, exact}));
   const dim3 grid(cdiv(a.n, rows), (unsigned)std::min(16, std::max(1, items / (4 * THREADS))));
   const size_t lds = (size_t)rows * half * sizeof(float2);
-  if (a.interleaved) hipLaunchKernelGGL((rotary_kernel<BF16, V, true>), grid, dim3(THREADS), lds, st, a, rows, divisor(head_items), divisor(items));
-  else hipLaunchKernelGGL((rotary_kernel<BF16, V, false>), grid, dim3(THREADS), lds, st, a, rows, divisor(head_items), divisor(items));
+  if (a.interleaved) hipLaunchKernelGGL((rotary_kernel<BF16, V, true>), grid, dim3(THREADS), lds, st, a, rows, divisor(items, head_items), divisor((int64_t)rows * items, items));
+  else hipLaunchKernelGGL((rotary_kernel<BF16, V, false>), grid, dim3(THREADS), lds, st, a, rows, divisor(items, head_items), divisor((int64_t)rows * items, items));
 }
 
 }  // namespace

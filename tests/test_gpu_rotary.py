@@ -42,6 +42,18 @@ CASES = [  # n, heads, hd, rot, interleaved, inverse, columns of x, of out, in p
 ]
 
 
+MANY_HEADS = [  # rows of more accesses than the square root of 2^32, where a quotient by a 32-bit reciprocal is no longer exact by itself
+    (3, 4095, 128, 2, True, False, 524160, 524160, False), (2, 3001, 128, 24, False, False, 384128, 384131, False), (2050, 733, 128, 2, False, False, 93824, 93825, False),
+    (3, 4093, 64, 2, False, True, 261952, 261953, True),
+]
+
+
+@pytest.mark.parametrize("bf16", [True, False])
+@pytest.mark.parametrize("case", MANY_HEADS, ids=lambda c: "-".join(map(str, c)))
+def test_rows_of_many_heads(torch_mod, bf16, case):
+    test_against_the_definition(torch_mod, bf16, case)
+
+
 @pytest.mark.parametrize("bf16", [True, False])
 @pytest.mark.parametrize("case", CASES, ids=lambda c: "-".join(map(str, c)))
 def test_against_the_definition(torch_mod, bf16, case):
