@@ -6,8 +6,8 @@
 // histogram, and then every wave lists its holes and displaced tokens.  With few requests the instructions of these passes set the time (a block a CU, one head of
 // 32768 tokens), so a pass does as little as it can: no token is compared with the length (key 0 is none), ties are counted only where some of them go, and the waves'
 // lists stay apart: whoever moves finds the i-th hole by the waves' counts.  The moves follow in the same launch or, for long lists, in one of their own
-// that the whole chip takes part in.  (8 requests x 8 heads of 32768 tokens of 128: 25 us and 47 of moves, the floor of all bytes 27; with the keys read again in
-// every pass, as beyond MAX_HELD tokens, 45 and 47.  32 heads of 512 and less: 12.6 us, a chain of passes with a barrier each.)
+// that the whole chip takes part in.  (8 requests x 8 heads of 20000 to 32768 tokens of 128, 12000 kept: 25 us and 47 of moves; the whole call 81, and 103 with the
+// keys read again in every pass, as beyond MAX_HELD tokens.  32 x 8 heads of 1025 to 1088: 12.6 us, a chain of passes with a barrier each.)
 #include "kernels.h"
 
 #include <algorithm>
