@@ -8,7 +8,7 @@
 // (i, g) = (lane % 16, lane / 16) holds row i and, with the tokens of the four S^T tiles chosen as 16 (i / 4) + 4 j + i % 4, the probabilities of tokens 16 g .. 16 g + 15,
 // which is the order in which a transposing LDS read hands out 16 tokens of a channel of V.  K: a lane's elements (32 of a 128-wide head, 16 of a 64-wide one)
 // lie in one group, so its scale goes into the conversion to bf16.  V: the scale belongs to a token, which is the reduction index, so it goes into P, once
-// for every 32 channels.  Both conversions are exact; P is rounded to bf16 (half a step, 2^-9 of each term) for bf16 rows and split into three
+// for every 32 channels.  Both conversions are exact; P is rounded to bf16 (half a step, 2^-8 of each term) for bf16 rows and split into three
 // terms (24 bits) for fp32 rows, as q is.  Sums, maxima and the output before its rounding are fp32.
 #include "kernels.h"
 #include "kv4.h"
@@ -439,24 +439,139 @@ __global__ __launch_bounds__(64 * WAVES, TERMS == 1 && HD == 64 ? 4 : 2) void kv
 // so that P needs no scaling and a transposing read of 4 tokens x 16 channels hands out V^T.  A value group that is NaN counts as 0 there and is noted beside it: only the
 // rows that see the token become NaN.  A turn's codes are asked for two turns ahead, put into LDS one ahead, their
 // blocks looked up three ahead.
-constexpr int ROW_TILES = 2, BLOCK_ROWS = WAVES * ROW_TILES * ROWS;
+constexpr int ROW_TILES = 2, BLOCK_ROWS = WAVES * ROW_TILES * ROWS, LEAST_TURNS = 4, NEAR = 2;
 typedef __attribute__((ext_vector_type(4))) short s16x4_t;
 typedef __attribute__((address_space(3))) s16x4_t lds_s16x4_t;
 
+// The work of a kv head, the turns of all blocks of rows of all requests one after the other, is cut into equal shares, one a thread block, since lengths and rows are known on the device only and
+// differ (a grid of requests, blocks of rows and equal splits of the longest context leaves the chip half idle: 6 requests of 134 to 238 rows at 2500 to 6700 tokens, 8 kv heads of 128, 168 us
+// with the joins, now 145; 64 of 5 to 60 rows at 500 to 6000 335, now 220).  A block of rows that is cut leaves states that
+// kv4_rows_join_kernel joins; a cut NEAR turns or less from the rows' begin or end, the price of one, moves there.
+struct Shares {
+  float *acc;                        // [Hkv, workers, 2, BLOCK_ROWS, HD] what a worker leaves of the rows that it began with in their middle and of those that it left before their end
+  float2 *ml;                        // [Hkv, workers, 2, BLOCK_ROWS]
+  float *lse2;
+  int4 *start;                       // [Hkv, workers] request, block of rows, turn in it (0: nothing cut)
+  int workers;
+};
+// Turns of the blocks of rows of a request.  (Rows that see nothing have some as well: they are written.)
+struct Turns {
+  int ctx, n, shift, tiles;          // 1 << shift: queries a block of rows
+  __device__ __forceinline__ Turns(const Kv4Attention &a, const Rows &w) : ctx(max(w.ctx, 0)), n(w.n), shift(__builtin_ctz(BLOCK_ROWS) - a.gshift), tiles((w.n + (1 << shift) - 1) >> shift) {}
+  __device__ __forceinline__ int of(int tile) const { return (ctx + min((tile + 1) << shift, n) + TURN - 1) / TURN; }
+  // of blocks 0 .. m - 1; (ctx + 63 + (k + 1) 2^shift) / 64 for a whole block k.  (Below 2^31; what is subtracted on the way may wrap.)
+  __device__ __forceinline__ uint32_t before(int m) const { return m == 0 ? 0u : m == tiles ? before_whole(m - 1) + (uint32_t)of(m - 1) : before_whole(m); }
+  __device__ __forceinline__ uint32_t before_whole(uint32_t m) const {
+    constexpr int TS = __builtin_ctz(TURN);
+    if (shift >= TS) return m * ((uint32_t)(ctx + TURN - 1) >> TS) + (half_product(m) << (shift - TS));
+    const uint32_t u = (uint32_t)(ctx + TURN - 1) >> shift;
+    return quotients(u + m, TS - shift) - quotients(u, TS - shift);
+  }
+  static __device__ __forceinline__ uint32_t half_product(uint32_t m) { return m % 2 ? (m + 1) / 2 * m : m / 2 * (m + 1); }      // m (m + 1) / 2
+  static __device__ __forceinline__ uint32_t quotients(uint32_t y, int s) {                                                       // sum of j >> s, j = 0 .. y
+    const uint32_t q = (y + 1) >> s;
+    return (half_product(q - 1) << s) + q * (y + 1 - (q << s));
+  }
+};
+
 template <int HD>
-__global__ __launch_bounds__(64 * WAVES, 2) void kv4_rows_kernel(Kv4Attention a, States x) {
+__global__ __launch_bounds__(64 * WAVES, 2) void kv4_rows_kernel(Kv4Attention a, Shares x) {
   constexpr int NS = HD / 32, NG = HD / 32, CT = HD / 16, VROW = HD * 2, KROW = HD / 2;
   __shared__ __align__(16) unsigned char sv[2][TURN * VROW], sk[2][TURN * KROW], sks[2][TURN * NG];
   __shared__ int any[3];                               // by turn, as the next two: read in it, filled in the one before, cleared in the one before that
   __shared__ unsigned long long nan[3][NG], missing[3];
-  const int kvh = blockIdx.x % a.c.Hkv, tile = gridDim.x / a.c.Hkv - 1 - blockIdx.x / a.c.Hkv, split = blockIdx.y;      // long tiles first; the tiles of a kv head on one XCD where there are 8 heads
-  const Rows w = rows_of<BLOCK_ROWS>(a, blockIdx.z, kvh, tile);
-  if (w.m0 >= w.m1) return;
-  const int end = w.ctx + query_of(a, w.m1 - 1) + 1, c0 = split * x.chunk, c1 = min(end, c0 + x.chunk);
-  if (c0 >= end && split > 0) return;
+  __shared__ int sums[WAVES];
+  __shared__ int4 cuts[2];                             // request, block of rows, turn in it, turns of all before
+  const int kvh = blockIdx.x % a.c.Hkv, worker = blockIdx.x / a.c.Hkv;      // (the workers of a kv head on one XCD where there are 8 heads)
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i = lane & 15, g = lane >> 4;
-  const int32_t *table = a.tables + (size_t)w.req * a.max_blocks;
   const float sc = score_scale(a);
+
+  // Where this share begins and the next one does: each thread adds up some requests, the one in whose part a cut falls finds the request, wave k the k-th cut's block of rows.
+  int left, req, tile, turn0 = 0;
+  if (x.workers > 0) {
+    const int per = (a.n_req + 64 * WAVES - 1) / (64 * WAVES), r0 = min(tid * per, a.n_req), r1 = min(r0 + per, a.n_req);
+    int mine = 0;
+    for (int r = r0; r < r1; ++r) {
+      const Turns w(a, rows_of<BLOCK_ROWS>(a, r, kvh, 0));
+      mine += (int)w.before(w.tiles);
+    }
+    int upto = mine;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int y = __shfl_up(upto, o, 64);
+      if (lane >= o) upto += y;
+    }
+    if (lane == 63) sums[wave] = upto;
+    __syncthreads();
+    int total = 0;
+#pragma unroll
+    for (int k = 0; k < WAVES; ++k) {
+      if (k < wave) upto += sums[k];
+      total += sums[k];
+    }
+    const int shares = min(x.workers, (total + LEAST_TURNS - 1) / LEAST_TURNS);
+    auto cut_of = [&](int k) { return k < shares ? (int)((double)total * k / shares) : total; };      // (exact before it is cut off: a product below 2^53, a quotient by less than 2^10)
+    for (int k = 0; k < 2; ++k) {
+      const int at = cut_of(worker + k);
+      if (at < upto - mine || at >= upto) continue;
+      int rest = at - (upto - mine);
+      for (int r = r0; r < r1; ++r) {
+        const Turns w(a, rows_of<BLOCK_ROWS>(a, r, kvh, 0));
+        const int here = (int)w.before(w.tiles);
+        if (rest < here) {
+          cuts[k] = make_int4(r, 0, rest, 0);
+          break;
+        }
+        rest -= here;
+      }
+    }
+    __syncthreads();
+    if (wave < 2) {
+      const int at = cut_of(worker + wave);
+      int4 in = make_int4(0, 0, 0, total);
+      if (at < total) {
+        const int r = __builtin_amdgcn_readfirstlane(cuts[wave].x), rest = cuts[wave].z;
+        const Turns w(a, rows_of<BLOCK_ROWS>(a, r, kvh, 0));
+        int b = 0;
+        for (int step = w.tiles > 64 ? 64 : 1;; step = 1) {
+          const int m = b + (lane + 1) * step;
+          b += step * __popcll(__ballot(m < w.tiles && (int)w.before(min(m, w.tiles)) <= rest));
+          if (step == 1) break;
+        }
+        const int turn = rest - (int)w.before(b), behind = w.of(b) - turn, near = min(NEAR, total / (8 * shares));
+        const int by = turn <= near ? -turn : behind <= near ? behind : 0;
+        in = make_int4(r, by > 0 ? b + 1 : b, by ? 0 : turn, at + by);
+      }
+      if (lane == 0) cuts[wave] = in;
+    }
+    __syncthreads();
+    const int4 in = cuts[0];
+    left = __builtin_amdgcn_readfirstlane(cuts[1].w - in.w);
+    req = __builtin_amdgcn_readfirstlane(in.x);
+    tile = __builtin_amdgcn_readfirstlane(in.y);
+    turn0 = __builtin_amdgcn_readfirstlane(in.z);
+    if (tid == 0) x.start[kvh * x.workers + worker] = left > 0 ? in : make_int4(0, 0, 0, 0);
+    if (left <= 0) return;
+  } else {
+    req = blockIdx.y;
+    tile = gridDim.x / a.c.Hkv - 1 - worker;           // long ones first
+    const Rows w = rows_of<BLOCK_ROWS>(a, req, kvh, tile);
+    if (w.m0 >= w.m1) return;
+    left = Turns(a, w).of(tile);
+  }
+
+  for (;; ++tile, turn0 = 0) {
+  Rows w = rows_of<BLOCK_ROWS>(a, req, kvh, tile);
+  while (w.m0 >= w.m1) {                               // behind the last rows of a request
+    if (++req >= a.n_req) return;
+    tile = 0;
+    w = rows_of<BLOCK_ROWS>(a, req, kvh, 0);
+  }
+  const int turns = Turns(a, w).of(tile), turn1 = min(turns, turn0 + left);
+  const bool cut = turn0 > 0 || turn1 < turns;
+  const int c0 = turn0 * TURN, c1 = min(w.ctx + query_of(a, w.m1 - 1) + 1, turn1 * TURN);
+  const int32_t *table = a.tables + (size_t)w.req * a.max_blocks;
+  __syncthreads();                                     // nobody reads the rows before any more
 
   // thread (token tid / NG, group tid % NG) of a turn (64-wide heads: the first 128 threads)
   const int vt = tid / NG, vg = tid % NG;
@@ -531,15 +646,21 @@ __global__ __launch_bounds__(64 * WAVES, 2) void kv4_rows_kernel(Kv4Attention a,
     if (t0 < wave_end) {
       const int marked = any[turn];
       f32x4_t s[ROW_TILES][4];
+      KCodes<HD> k[4];
+      uint32_t ks[4];
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const float ks = kv4::scale_value(sks[buf][(16 * j + i) * NG + g * (HD / 4) / kv4::GROUP]);
-        const KCodes<HD> k = load_k<HD, false>(sk[buf] + (16 * j + i) * KROW + g * (KROW / 4));
+        ks[j] = sks[buf][(16 * j + i) * NG + g * (HD / 4) / kv4::GROUP];
+        k[j] = load_k<HD, false>(sk[buf] + (16 * j + i) * KROW + g * (KROW / 4));
+      }
+      __builtin_amdgcn_sched_barrier(0);                 // (all keys read before the first product, as the values below)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
 #pragma unroll
         for (int b = 0; b < ROW_TILES; ++b) s[b][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int st = 0; st < NS; ++st) {
-          const bf16x8_t kf = kv4::decode8(k.w[st], ks);
+          const bf16x8_t kf = kv4::decode8(k[j].w[st], kv4::scale_value(ks[j]));
 #pragma unroll
           for (int b = 0; b < ROW_TILES; ++b) s[b][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, q[b][0][st], s[b][j], 0, 0, 0);
         }
@@ -619,7 +740,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void kv4_rows_kernel(Kv4Attention a,
     if (mr >= w.m1) continue;
     const int k = query_of(a, mr), head = head_of(a, kvh, mr), Hq = a.c.Hkv * a.group;
     const size_t r = w.row0 + k, at = row_id(a, w.req, k, head);
-    if (x.nsplit == 1) {
+    if (!cut) {
       const float inv = l == 0.f ? 0.f : 1.f / l;
       bf16_t *to = (bf16_t *)a.out + r * a.ld_out + (size_t)head * HD + 4 * g;
 #pragma unroll
@@ -630,43 +751,40 @@ __global__ __launch_bounds__(64 * WAVES, 2) void kv4_rows_kernel(Kv4Attention a,
         if (a.add_weight) x.lse2[at] = lse2;
       }
     } else {
-      float *to = x.acc + (at * x.nsplit + split) * HD + 4 * g;
+      const size_t state = (((size_t)kvh * x.workers + worker) * 2 + (turn0 == 0)) * BLOCK_ROWS + (mr - w.m0);
+      float *to = x.acc + state * HD + 4 * g;
 #pragma unroll
       for (int c = 0; c < CT; ++c) *(f32x4_t *)(to + 16 * c) = o[b][c];
-      if (g == 0) x.ml[at * x.nsplit + split] = make_float2(sx[b].top, l);
+      if (g == 0) x.ml[state] = make_float2(sx[b].top, l);
     }
+  }
+  left -= turn1 - turn0;
+  if (left <= 0) return;
   }
 }
 
 // Joins the splits of a row and head: `groups` teams of HD / 4 lanes (four channels each) take every groups-th split with a soft-max state of their own and are merged
 // in order.  The time is the latency of the loads, so a team has those of IN_FLIGHT splits under way.
 constexpr int IN_FLIGHT = 4;
-template <int HD, bool BF16>
-__device__ __forceinline__ void join_rows(const Kv4Attention &a, const States &x, int block, int groups, bool keep_lse2, float4 *so, float2 *sml) {
-  constexpr int LANES = HD / 4;
-  const int Hq = a.c.Hkv * a.group, team = threadIdx.x / LANES, e = threadIdx.x % LANES, grp = team % groups;
-  const size_t at = (size_t)block * (64 * WAVES / LANES / groups) + team / groups, rows = (size_t)a.n_req * a.max_rows * Hq;
-  const int head = (int)(at % Hq), k = (int)(at / Hq % a.max_rows), req = (int)(min(at, rows - 1) / Hq / a.max_rows);
-  const Rows w = rows_of<1>(a, req, head >> a.gshift, 0);
-  const bool live = at < rows && k < w.n;
-  const int ns = live ? splits_of(a, x, w, k, head) : 0;
-  const float *acc = x.acc + at * x.nsplit * HD;
-  const float2 *ml = x.ml + at * x.nsplit;
-  float mn = -INFINITY, ls = 0.f;
-  float4 as = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int s0 = grp; s0 < ns; s0 += IN_FLIGHT * groups) {
+// Merges states first, first + step, .. below n, of which s lies at place(s): channels 4 e .. + 3.
+template <int HD, class Place>
+__device__ __forceinline__ void merge(const float *acc, const float2 *ml, int first, int n, int step, int e, Place place, float &mn, float &ls, float4 &as) {
+  mn = -INFINITY;
+  ls = 0.f;
+  as = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int s0 = first; s0 < n; s0 += IN_FLIGHT * step) {
     float4 v[IN_FLIGHT];
     float2 y[IN_FLIGHT];
 #pragma unroll
     for (int u = 0; u < IN_FLIGHT; ++u) {
-      const int s = min(s0 + u * groups, ns - 1);
-      y[u] = ml[s];
-      v[u] = ((const float4 *)(acc + (size_t)s * HD))[e];
+      const size_t at = place(min(s0 + u * step, n - 1));
+      y[u] = ml[at];
+      v[u] = ((const float4 *)(acc + at * HD))[e];
     }
     float top = mn;
 #pragma unroll
     for (int u = 0; u < IN_FLIGHT; ++u) {
-      if (s0 + u * groups >= ns) { y[u] = make_float2(-INFINITY, 0.f); v[u] = make_float4(0.f, 0.f, 0.f, 0.f); }
+      if (s0 + u * step >= n) { y[u] = make_float2(-INFINITY, 0.f); v[u] = make_float4(0.f, 0.f, 0.f, 0.f); }
       top = fmaxf(top, y[u].x);
     }
     const float base = top == -INFINITY ? 0.f : top, old = __builtin_amdgcn_exp2f(mn - base);
@@ -680,6 +798,32 @@ __device__ __forceinline__ void join_rows(const Kv4Attention &a, const States &x
       as.x += v[u].x * f; as.y += v[u].y * f; as.z += v[u].z * f; as.w += v[u].w * f;
     }
   }
+}
+// Writes channels 4 e .. + 3 of row r of the output and, by e = 0, its log sum; keep: where the weights read it, or null.
+template <int HD, bool BF16>
+__device__ __forceinline__ void put_joined(const Kv4Attention &a, size_t r, int head, int e, float mn, float ls, const float4 &as, float *keep) {
+  const float inv = ls == 0.f ? 0.f : 1.f / ls;
+  const size_t to = r * a.ld_out + (size_t)head * HD + 4 * e;
+  if constexpr (BF16) *(uint2 *)((bf16_t *)a.out + to) = make_uint2(cvt_pk_bf16(as.x * inv, as.y * inv), cvt_pk_bf16(as.z * inv, as.w * inv));
+  else *(float4 *)((float *)a.out + to) = make_float4(as.x * inv, as.y * inv, as.z * inv, as.w * inv);
+  if (e == 0) {
+    const float lse2 = ls == 0.f ? -INFINITY : mn + log2f(ls);
+    if (a.lse) a.lse[r * (a.c.Hkv * a.group) + head] = lse2 / LOG2E;
+    if (keep) *keep = lse2;
+  }
+}
+template <int HD, bool BF16>
+__device__ __forceinline__ void join_rows(const Kv4Attention &a, const States &x, int block, int groups, bool keep_lse2, float4 *so, float2 *sml) {
+  constexpr int LANES = HD / 4;
+  const int Hq = a.c.Hkv * a.group, team = threadIdx.x / LANES, e = threadIdx.x % LANES, grp = team % groups;
+  const size_t at = (size_t)block * (64 * WAVES / LANES / groups) + team / groups, rows = (size_t)a.n_req * a.max_rows * Hq;
+  const int head = (int)(at % Hq), k = (int)(at / Hq % a.max_rows), req = (int)(min(at, rows - 1) / Hq / a.max_rows);
+  const Rows w = rows_of<1>(a, req, head >> a.gshift, 0);
+  const bool live = at < rows && k < w.n;
+  const int ns = live ? splits_of(a, x, w, k, head) : 0;
+  float mn, ls;
+  float4 as;
+  merge<HD>(x.acc, x.ml, grp, ns, groups, e, [&](int s) { return at * x.nsplit + s; }, mn, ls, as);
   if (groups > 1) {
     so[threadIdx.x] = as;
     if (e == 0) sml[team] = make_float2(mn, ls);
@@ -698,16 +842,7 @@ __device__ __forceinline__ void join_rows(const Kv4Attention &a, const States &x
     }
   }
   if (!live || grp) return;
-  const float inv = ls == 0.f ? 0.f : 1.f / ls;
-  const size_t r = w.row0 + k;
-  const size_t to = r * a.ld_out + (size_t)head * HD + 4 * e;
-  if constexpr (BF16) *(uint2 *)((bf16_t *)a.out + to) = make_uint2(cvt_pk_bf16(as.x * inv, as.y * inv), cvt_pk_bf16(as.z * inv, as.w * inv));
-  else *(float4 *)((float *)a.out + to) = make_float4(as.x * inv, as.y * inv, as.z * inv, as.w * inv);
-  if (e == 0) {
-    const float lse2 = ls == 0.f ? -INFINITY : mn + log2f(ls);
-    if (a.lse) a.lse[r * Hq + head] = lse2 / LOG2E;
-    if (keep_lse2) x.lse2[at] = lse2;
-  }
+  put_joined<HD, BF16>(a, (size_t)w.row0 + k, head, e, mn, ls, as, keep_lse2 ? x.lse2 + at : nullptr);
 }
 
 template <int HD, bool BF16>
@@ -715,6 +850,29 @@ __global__ __launch_bounds__(64 * WAVES) void kv4_join_kernel(Kv4Attention a, St
   __shared__ float4 so[64 * WAVES];
   __shared__ float2 sml[64 * WAVES / (HD / 4)];
   join_rows<HD, BF16>(a, x, blockIdx.x, groups, a.add_weight, so, sml);
+}
+
+// Joins what the workers of a kv head left of the rows that they cut: block (worker, head, part of the rows) does so for the rows that the worker begins in the middle of, if it is the
+// first to do so; the others of the same rows follow it.
+template <int HD>
+__global__ __launch_bounds__(64 * WAVES) void kv4_rows_join_kernel(Kv4Attention a, Shares x) {
+  constexpr int LANES = HD / 4;
+  const int worker = blockIdx.x + 1, kvh = blockIdx.y, e = threadIdx.x % LANES;
+  const int4 *starts = x.start + kvh * x.workers, start = starts[worker];
+  auto same = [&](const int4 &y) { return y.x == start.x && y.y == start.y && y.z > 0; };
+  if (start.z == 0 || same(starts[worker - 1])) return;
+  int n = 2;                         // with the worker before
+  while (worker + n - 1 < x.workers && same(starts[worker + n - 1])) ++n;
+  const Rows w = rows_of<BLOCK_ROWS>(a, start.x, kvh, start.y);
+  const int row = blockIdx.z * (64 * WAVES / LANES) + threadIdx.x / LANES, m = w.m0 + row;
+  if (m >= w.m1) return;
+  const int k = query_of(a, m), head = head_of(a, kvh, m);
+  const size_t before = (((size_t)kvh * x.workers + worker - 1) * 2 + 1) * BLOCK_ROWS + row;
+  float mn, ls;
+  float4 as;
+  // the worker before left the second of its two, the others the first
+  merge<HD>(x.acc, x.ml, 0, n, 1, e, [&](int s) { return s == 0 ? before : before + (size_t)(2 * s - 1) * BLOCK_ROWS; }, mn, ls, as);
+  put_joined<HD, true>(a, (size_t)w.row0 + k, head, e, mn, ls, as, a.add_weight ? x.lse2 + row_id(a, w.req, k, head) : nullptr);
 }
 
 // Adds every token's probabilities, summed over the rows of its request and the query heads of its kv head, to its weight, from the product S = Q K^T formed again
@@ -863,10 +1021,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void kv4_weight_rows_kernel(Kv4Atten
     for (int st = 0; st < NS; ++st) kf[j][st] = kv4::decode8(k.w[st], ks);
   }
   store(0);
-  int buf = 0;
-  for (int m0 = first; m0 < n_rows; m0 += STAGE, buf ^= 1) {
-    __syncthreads();
-    if (m0 + STAGE < n_rows) load(m0 + STAGE);
+  auto stage = [&](int m0, int buf, auto masked) {
 #pragma unroll
     for (int r0 = 0; r0 < STAGE; r0 += ROWS) {         // (behind the last row: nothing is added)
       bf16x8_t q[TERMS][NS];
@@ -875,7 +1030,6 @@ __global__ __launch_bounds__(64 * WAVES, 2) void kv4_weight_rows_kernel(Kv4Atten
 #pragma unroll
         for (int st = 0; st < NS; ++st) q[t][st] = __builtin_bit_cast(bf16x8_t, sq[buf][t][(r0 + i) * CPR + ((g * (CPR / 4) + st) ^ swizzle(i))]);
       const f32x4_t ls = *(const f32x4_t *)(slse[buf] + r0 + 4 * g);
-      const bool whole = t0 + TURN <= w.ctx + query_of(a, m0 + r0) + 1;
       f32x4_t s[4];
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
@@ -885,7 +1039,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void kv4_weight_rows_kernel(Kv4Atten
 #pragma unroll
           for (int t = TERMS - 1; t >= 0; --t) s[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(q[t][st], kf[j][st], s[j], 0, 0, 0);
       }
-      if (!whole) {
+      if constexpr (masked) {
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           const int last = w.ctx + query_of(a, m0 + r0 + 4 * g + r) + 1 - t0 - i;      // the row sees tokens below it
@@ -898,6 +1052,14 @@ __global__ __launch_bounds__(64 * WAVES, 2) void kv4_weight_rows_kernel(Kv4Atten
 #pragma unroll
         for (int r = 0; r < 4; ++r) sum[j] += __builtin_amdgcn_exp2f(fmaf(s[j][r], sc, -ls[r]));
     }
+  };
+  int buf = 0;
+  for (int m0 = first; m0 < n_rows; m0 += STAGE, buf ^= 1) {
+    __syncthreads();
+    if (m0 + STAGE < n_rows) load(m0 + STAGE);
+    // one branch for a stage, not for its tiles, so that the products of a tile run beside the exponentials of the one before
+    if (t0 + TURN <= w.ctx + query_of(a, m0) + 1) stage(m0, buf, std::false_type{});
+    else stage(m0, buf, std::true_type{});
     if (m0 + STAGE < n_rows) store(buf ^ 1);
   }
 #pragma unroll
@@ -920,18 +1082,23 @@ int chunk_tokens(int n_req, int tiles, int Hkv, int tokens) {
 // Rows of a kv head up to which the first kernel takes bf16 requests, tile by tile; us on it and on the kernel of many rows, 64 requests of 2000 tokens, 8 kv heads: 16 / 24 / 32 rows
 // of 128-wide heads 45 and 62 / 66 and 63 / 67 and 63, 32 / 48 / 64 rows of 64-wide ones 40 and 49 / 56 and 62 / 73 and 63.
 int few_rows(int hd) { return hd == 128 ? 16 : 48; }
-// Two blocks a CU, or splits of four turns.
-int rows_chunk(int n_req, int tiles, int Hkv, int tokens) {
-  const long long blocks = (long long)n_req * Hkv * tiles;
-  const int nsplit = (int)std::max(1ll, std::min<long long>(cdiv(tokens, 4 * TURN), (512 + blocks - 1) / blocks));
-  return cdiv(cdiv(tokens, nsplit), TURN) * TURN;
+// Thread blocks of a kv head for shares: two a CU in all, or as many as there can be shares of LEAST_TURNS.  0: the blocks of rows are the thread blocks, long ones first, nothing is cut and
+// nothing joined.  That is for many of them, or for two rounds of them that come from long pieces, whose blocks are alike; few rows a request, of any lengths, need shares.  us by blocks
+// and by shares, 8 kv heads of 128: a piece of 4096 rows behind 4096 tokens 439 and 483, three of 600 to 2000 rows 135 and 159; 96 requests of 5 to 60 rows at 500 to 6000 tokens 488 and 340,
+// 120 of them 561 and 407 (16 of 256 rows at 4000 each, 32 heads: 377 and 398).
+constexpr int ENOUGH = 2000, ENOUGH_ALIKE = 1024, ALIKE = 16;
+int workers_of(int n_req, int tiles, int Hkv, int tokens) {
+  const long long blocks = (long long)n_req * tiles, turns = blocks * cdiv(tokens, TURN);
+  if (blocks * Hkv >= (tiles >= ALIKE ? ENOUGH_ALIKE : ENOUGH)) return 0;
+  return (int)std::max(1ll, std::min<long long>(512 / Hkv, (turns + LEAST_TURNS - 1) / LEAST_TURNS));
 }
+static_assert(ENOUGH * (((1ll << 26) + 65535) / TURN + 1) < INT32_MAX, "turns of a kv head");
 // Copies of a row in a tile: as many as rows and scale groups leave room for.
 int copies(int rows, int hd) { return rows <= 4 && hd == 128 ? 4 : rows <= 8 ? 2 : 1; }
 
 struct Plan {
-  bool many;                 // blocks of many rows
-  int rep, tile_rows, tiles, nsplit, chunk;
+  bool many;                 // blocks of many rows, by `workers` a kv head
+  int rep, tile_rows, tiles, nsplit, chunk, workers;
   size_t rows;
 };
 Plan plan_of(int n_req, int max_rows, int max_context, int Hq, int Hkv, int hd, bool bf16) {
@@ -941,20 +1108,31 @@ Plan plan_of(int n_req, int max_rows, int max_context, int Hq, int Hkv, int hd, 
   p.rep = copies(rows, hd);
   p.tile_rows = p.many ? BLOCK_ROWS : ROWS / p.rep;
   p.tiles = cdiv(rows, p.tile_rows);
-  p.chunk = p.many ? rows_chunk(n_req, p.tiles, Hkv, tokens) : chunk_tokens(n_req, p.tiles, Hkv, tokens);
+  p.workers = workers_of(n_req, p.tiles, Hkv, tokens);
+  p.chunk = chunk_tokens(n_req, p.tiles, Hkv, tokens);
   p.nsplit = cdiv(tokens, p.chunk);
   p.rows = (size_t)n_req * max_rows * Hq;
   return p;
 }
-// (acc is there for several splits only)
-size_t ml_bytes(const Plan &p) { return align_up(p.rows * p.nsplit * sizeof(float2), 256); }
-size_t lse_bytes(const Plan &p) { return align_up(p.rows * sizeof(float), 256); }
+// A workspace: log sums of all rows, states of few rows (acc for several splits only) or shares and what they leave.
+struct Layout {
+  size_t lse2, ml, start, acc, bytes;
+};
+Layout layout_of(const Plan &p, int Hkv, int hd) {
+  Layout l;
+  const size_t states = p.many ? (size_t)Hkv * p.workers * 2 * BLOCK_ROWS : p.rows * p.nsplit;
+  l.lse2 = 0;
+  l.ml = align_up(p.rows * sizeof(float), 256);
+  l.start = l.ml + align_up(states * sizeof(float2), 256);
+  l.acc = l.start + (p.many ? align_up((size_t)Hkv * p.workers * sizeof(int4), 256) : 0);
+  l.bytes = l.acc + (p.many || p.nsplit > 1 ? states * hd * sizeof(float) : 0);
+  return l;
+}
 
 }  // namespace
 
 size_t kv4_attention_scratch_bytes(int n_req, int max_rows, int max_context, int Hq, int Hkv, int hd, bool bf16) {
-  const Plan p = plan_of(n_req, max_rows, max_context, Hq, Hkv, hd, bf16);
-  return ml_bytes(p) + lse_bytes(p) + (p.nsplit > 1 ? p.rows * p.nsplit * hd * sizeof(float) : 0);
+  return layout_of(plan_of(n_req, max_rows, max_context, Hq, Hkv, hd, bf16), Hkv, hd).bytes;
 }
 
 hipError_t launch_kv4_attention(const Kv4Attention &a, bool bf16, void *scratch, hipStream_t st) {
@@ -963,12 +1141,17 @@ hipError_t launch_kv4_attention(const Kv4Attention &a, bool bf16, void *scratch,
   const Plan p = plan_of(a.n_req, a.max_rows, a.max_context, Hkv * a.group, Hkv, hd, bf16);
   const bool runs = a.c.bshift >= 4;
   char *at = (char *)scratch;
-  const States x = {(float *)(at + ml_bytes(p) + lse_bytes(p)), (float2 *)at, (float *)(at + ml_bytes(p)), p.nsplit, p.chunk, p.tile_rows};
+  const Layout l = layout_of(p, Hkv, hd);
+  const States x = {(float *)(at + l.acc), (float2 *)(at + l.ml), (float *)(at + l.lse2), p.nsplit, p.chunk, p.tile_rows};
+  const Shares shares = {(float *)(at + l.acc), (float2 *)(at + l.ml), (float *)(at + l.lse2), (int4 *)(at + l.start), p.workers};
   auto main = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(Hkv * p.tiles, p.nsplit, a.n_req), dim3(64 * WAVES), 0, st, a, x, p.tiles); };
-  auto many = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(Hkv * p.tiles, p.nsplit, a.n_req), dim3(64 * WAVES), 0, st, a, x); };
+  auto many = [&](auto kernel, auto join) {
+    hipLaunchKernelGGL(kernel, p.workers ? dim3(Hkv * p.workers) : dim3(Hkv * p.tiles, a.n_req), dim3(64 * WAVES), 0, st, a, shares);
+    if (p.workers > 1) hipLaunchKernelGGL(join, dim3(p.workers - 1, Hkv, BLOCK_ROWS * (hd / 4) / (64 * WAVES)), dim3(64 * WAVES), 0, st, a, shares);
+  };
   // teams of a row and head: one up to the splits that it has under way at once, else four or all of a block
   const int teams = 64 * WAVES / (hd / 4), groups = p.nsplit <= IN_FLIGHT ? 1 : p.nsplit <= 4 * IN_FLIGHT ? 4 : teams;
-  const int joins = p.nsplit > 1 ? (int)((p.rows * groups + teams - 1) / teams) : 0, pieces = cdiv(tokens, TURN * WAVES);
+  const int joins = !p.many && p.nsplit > 1 ? (int)((p.rows * groups + teams - 1) / teams) : 0, pieces = cdiv(tokens, TURN * WAVES);
   const bool one_tile = a.max_rows * a.group <= ROWS;
   auto join = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(joins), dim3(64 * WAVES), 0, st, a, x, groups); };
   auto weight = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(joins + Hkv * pieces * a.n_req), dim3(64 * WAVES), 0, st, a, x, joins, groups, pieces); };
@@ -977,7 +1160,7 @@ hipError_t launch_kv4_attention(const Kv4Attention &a, bool bf16, void *scratch,
     constexpr int T = decltype(terms)::value;
     constexpr bool R = decltype(in_runs)::value;
     if constexpr (T == 1) {
-      if (p.many) hd == 128 ? many(kv4_rows_kernel<128>) : many(kv4_rows_kernel<64>);
+      if (p.many) hd == 128 ? many(kv4_rows_kernel<128>, kv4_rows_join_kernel<128>) : many(kv4_rows_kernel<64>, kv4_rows_join_kernel<64>);
     }
     if (p.many) {}
     else if (hd == 128) p.rep == 4 ? main(kv4_attention_kernel<128, T, 4, R>) : p.rep == 2 ? main(kv4_attention_kernel<128, T, 2, R>) : main(kv4_attention_kernel<128, T, 1, R>);
