@@ -375,7 +375,7 @@ int mace_token_logprobs_grad(mace_handle_t h, const void *logits, int32_t dtype,
  *              ld_x, ld_out elements apart; columns behind them are neither read nor written.  Aligned to their elements (16-byte aligned rows and
  *              rot_dim / 2 a multiple of 16 bytes run fastest).  out may be x (same stride); else they do not overlap, judged from first to last element
  *   positions  device int32 [n], any value;  inv_freq  device fp64 [rot_dim / 2], any finite values of magnitude up to 2^19;  magnitude finite;  n_heads 1..4096
- * No workspace; one launch.  The device of mace_create must be current (MACE_INVALID_ARG otherwise; so for the calls below). */
+ * No workspace; one launch (beyond 2^23 rows perhaps several).  The device of mace_create must be current (MACE_INVALID_ARG otherwise; so for the calls below). */
 int mace_rotary_frequencies(int32_t rot_dim, double theta, double factor, int32_t original_len, double slow, double fast, double *inv_freq);
 int mace_rotary(mace_handle_t h, const void *x, int64_t ld_x, const int32_t *positions, const double *inv_freq, int32_t rot_dim, int32_t interleaved,
                 double magnitude, int32_t inverse, int32_t n, int32_t n_heads, void *out, int64_t ld_out, void *stream);
@@ -423,7 +423,7 @@ int mace_kv4_gather(mace_handle_t h, const mace_kv4_cache_t *cache, const int32_
  *                 cache->weight.  The bits are a function of the inputs, except in blocks that requests of the call share: there the requests' sums arrive in any order
  * Rows of q and out that no request has are neither read nor written.  Tokens of blocks outside the cache are left out; a row without any token has out 0 and
  * lse -inf.  What lies behind a request's last token in its blocks is never used, whatever it holds.  A NaN in a key makes the rows that attend to it NaN, in a value
- * their 32 columns.
+ * their 32 columns (a value whose probability is below 2^-126 of the row's largest may do so or not).
  * Precision: codes and scales are exact; q is exact; probabilities are rounded to bf16 before the product with V for bf16 models and carry 24 bits for fp32 ones; all
  * sums are fp32; out is rounded once.  workspace: mace_kv4_attention_workspace_bytes for the sizes of the call (other sizes can need more or less), 256-byte aligned,
  * nothing of it read before it is written.  Outputs and workspace overlap neither an input nor each other, judged from first to last element.

@@ -81,10 +81,21 @@ void launch(const Rotary &a, hipStream_t st) {
   const int half = a.rot / 2, copied = a.x == a.out ? 0 : (a.hd - a.rot) / (2 * V), head_items = half / V + copied, items = a.n_heads * head_items;
   const int exact = (int)std::min((1ll << 32) / ((long long)items * items), 2048ll);           // rows that `divisor` holds for
   const int rows = std::max(1, std::min({std::max(THREADS / half / 4, cdiv(2 * THREADS, items)), a.n / 1024, 2048 / half, exact}));
-  const dim3 grid(cdiv(a.n, rows), (unsigned)std::min(16, std::max(1, items / (4 * THREADS))));
+  const unsigned across = (unsigned)std::min(16, std::max(1, items / (4 * THREADS)));
   const size_t lds = (size_t)rows * half * sizeof(float2);
-  if (a.interleaved) hipLaunchKernelGGL((rotary_kernel<BF16, V, true>), grid, dim3(THREADS), lds, st, a, rows, divisor(items, head_items), divisor((int64_t)rows * items, items));
-  else hipLaunchKernelGGL((rotary_kernel<BF16, V, false>), grid, dim3(THREADS), lds, st, a, rows, divisor(items, head_items), divisor((int64_t)rows * items, items));
+  // (a grid has less than 2^32 threads in a direction: more rows go in several launches)
+  const int most = (int)std::min<long long>(INT32_MAX, (long long)rows << 23);
+  for (int r0 = 0; r0 < a.n; r0 += std::min(most, a.n - r0)) {
+    Rotary b = a;
+    const size_t es = BF16 ? 2 : 4;
+    b.x = (const char *)a.x + (size_t)r0 * a.ld_x * es;
+    b.out = (char *)a.out + (size_t)r0 * a.ld_out * es;
+    b.positions = a.positions + r0;
+    b.n = std::min(most, a.n - r0);
+    const dim3 grid(cdiv(b.n, rows), across);
+    if (a.interleaved) hipLaunchKernelGGL((rotary_kernel<BF16, V, true>), grid, dim3(THREADS), lds, st, b, rows, divisor(items, head_items), divisor((int64_t)rows * items, items));
+    else hipLaunchKernelGGL((rotary_kernel<BF16, V, false>), grid, dim3(THREADS), lds, st, b, rows, divisor(items, head_items), divisor((int64_t)rows * items, items));
+  }
 }
 
 }  // namespace

@@ -5,6 +5,7 @@ import pytest
 
 import kv4_reference as R
 from test_gpu_kv4_attention import check
+from test_gpu_kv4_cache import Model
 from test_gpu_kv4_evict import expected
 from test_gpu_rotary import reference
 
@@ -123,3 +124,101 @@ def test_whole_cache_is_near_the_unrounded_attention(torch_mod):
         assert ((got - want).abs() <= bound + 1e-5).all()
     finally:
         B.mace_destroy(h)
+
+
+def test_blocks_at_the_end_of_a_large_pool(torch_mod):
+    """The same tokens in a small pool and in the last blocks of one whose byte offsets pass 2^32: attention, weights and eviction have the same bits."""
+    torch = torch_mod
+    hkv, hd, size, blocks, used = 8, 128, 16, 1 << 20, 24
+    gen = torch.Generator().manual_seed(4)
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")
+    x = torch.randn((used * size, hkv * hd), generator=gen).to(torch.bfloat16).cuda()
+    order = torch.randperm(used, generator=gen)
+    with Model(hkv, hd, True, 2) as (B, h):
+        for count in (1, 20):                                           # few rows and many
+            got = []
+            for first, n in ((0, used), (blocks - used, blocks)):
+                pool = lambda b, t=torch.uint8: torch.zeros((n, hkv, size, b) if b else (n, hkv, size), dtype=t, device="cuda")
+                arrays = [pool(64), pool(64), pool(4), pool(4), pool(0, torch.float32), pool(0, torch.int32)]
+                s = B.kv4_cache_struct(*arrays)
+                slots = (first + order[torch.arange(used * size) // size]) * size + torch.arange(used * size) % size
+                B.mace_kv4_append(h, s, x, x.flip(0).contiguous(), slots.int().cuda(), positions=i32(list(range(used * size))))
+                table, lens = (first + order).int().cuda().view(1, used), i32([used * size - count])
+                q = torch.randn((count, 2 * hkv * hd), generator=torch.Generator().manual_seed(count)).to(torch.bfloat16).cuda()
+                out, work = torch.empty_like(q), lambda b: torch.empty(b, dtype=torch.uint8, device="cuda")
+                B.mace_kv4_attention(h, s, q, table, lens, out, work(B.mace_kv4_attention_workspace_bytes(h, 1, count, used * size)), used * size, q_offsets=i32([0, count]),
+                                     max_rows=count, add_weight=True)
+                new = torch.empty((1, hkv), dtype=torch.int32, device="cuda")
+                B.mace_kv4_evict(h, s, table, i32([used * size]), i32([used * size]), i32([[100] * hkv]), new, work(B.mace_kv4_evict_workspace_bytes(h, 1, used * size)), used * size, 4, 16)
+                torch.cuda.synchronize()
+                got.append([out.clone()] + [a[first:].clone() for a in arrays])
+                del arrays, s
+            assert (got[0][0] != 0).any() and (got[0][5] > 0).any()
+            assert all(torch.equal(a, b) for a, b in zip(*got))
+
+
+@pytest.mark.parametrize("max_rows,group,bf16", [(1, 1, True), (3, 4, False), (40, 2, True), (300, 4, True), (40, 2, False)])
+def test_nothing_behind_the_workspace_is_written(torch_mod, max_rows, group, bf16):
+    """Requests of all sizes up to the bounds, in a workspace of exactly the stated size and in one with bytes of every kind before the call: the same outputs, and the bytes behind stay."""
+    torch = torch_mod
+    hkv, hd, size, mc = 2, 64, 16, 5000
+    r = np.random.default_rng(max_rows)
+    i32 = lambda x: torch.from_numpy(np.ascontiguousarray(x, dtype=np.int32)).cuda()
+    with Model(hkv, hd, bf16, group) as (B, h):
+        n_req = 5
+        counts, lens = np.array([max_rows, 1, max_rows // 2, 0, max_rows]), np.array([mc, mc, 300, 70, 0])
+        cache = R.Cache(B, 700, hkv, size, hd, 1)
+        tables = np.stack([cache.request(int(l + c), -(-(mc + max_rows) // size)) for l, c in zip(lens, counts)])
+        s = cache.upload(B)
+        first = np.concatenate([[0], np.cumsum(counts)])
+        dtype = torch.bfloat16 if bf16 else torch.float32
+        q = torch.from_numpy(r.standard_normal((int(first[-1]), hkv * group * hd)).astype(np.float32)).to(dtype).cuda()
+        kept = {n: cache.dev[n].clone() for n in cache.dev}
+        results = []
+        for fill, budget in ((0x00, 1000), (0xFF, 1000), (0x7F, 1000)):
+            for n in kept:
+                cache.dev[n].copy_(kept[n])
+            size_a, size_e = B.mace_kv4_attention_workspace_bytes(h, n_req, max_rows, mc), B.mace_kv4_evict_workspace_bytes(h, n_req, mc)
+            wa, we = (torch.full((b + 4096,), fill, dtype=torch.uint8, device="cuda") for b in (size_a, size_e))
+            out, lse = torch.empty_like(q), torch.empty((q.shape[0], hkv * group), device="cuda")
+            B.mace_kv4_attention(h, s, q, i32(tables), i32(lens), out, wa[:size_a], mc, q_offsets=i32(first), max_rows=max_rows, lse=lse, add_weight=True)
+            new = torch.empty((n_req, hkv), dtype=torch.int32, device="cuda")
+            B.mace_kv4_evict(h, s, i32(tables), i32(lens), i32(lens), i32(np.full((n_req, hkv), budget)), new, we[:size_e], mc, 4, 16)
+            torch.cuda.synchronize()
+            assert (wa[size_a:] == fill).all() and (we[size_e:] == fill).all()
+            results.append([out, lse, new] + [cache.dev[n].view(torch.uint8).clone() for n in kept])
+        for other in results[1:]:
+            assert all(torch.equal(a.view(torch.uint8) if a.dtype != torch.int32 else a, b.view(torch.uint8) if b.dtype != torch.int32 else b) for a, b in zip(results[0], other))
+
+
+def test_scales_at_four_byte_alignment(torch_mod):
+    """k_scale, v_scale, weight and position may begin at any multiple of four bytes."""
+    torch = torch_mod
+    hkv, size = 2, 16
+    for hd in (64, 128):
+        with Model(hkv, hd, True, 4) as (B, h):
+            cache = R.Cache(B, 40, hkv, size, hd, 2)
+            table = cache.request(400, 25)[None]
+            s = cache.upload(B)
+            q = torch.randn((1, hkv * 4 * hd), generator=torch.Generator().manual_seed(0)).to(torch.bfloat16).cuda()
+
+            def go(s, count):
+                rows = q.repeat(count, 1)
+                out = torch.empty_like(rows)
+                work = torch.empty(B.mace_kv4_attention_workspace_bytes(h, 1, count, 400), dtype=torch.uint8, device="cuda")
+                B.mace_kv4_attention(h, s, rows, torch.from_numpy(table).cuda(), torch.tensor([400 - count], dtype=torch.int32, device="cuda"), out, work, 400,
+                                     q_offsets=torch.tensor([0, count], dtype=torch.int32, device="cuda"), max_rows=count, add_weight=True)
+                torch.cuda.synchronize()
+                return out
+
+            moved = {}
+            for n in ("k_scale", "v_scale", "weight", "position"):
+                raw = cache.dev[n].view(torch.uint8).flatten()
+                moved[n] = torch.empty(raw.numel() + 4, dtype=torch.uint8, device="cuda")[4:]
+                moved[n].copy_(raw)
+                moved[n] = moved[n].view(cache.dev[n].dtype).view(cache.dev[n].shape)
+                assert moved[n].data_ptr() % 16 == 4
+            s2 = B.kv4_cache_struct(cache.dev["k"], cache.dev["v"], moved["k_scale"], moved["v_scale"], moved["weight"], moved["position"])
+            for count in (1, 5, 60):
+                assert torch.equal(go(s, count), go(s2, count))
+            assert torch.equal(moved["weight"].view(torch.uint8), cache.dev["weight"].view(torch.uint8))

@@ -88,7 +88,7 @@ def test_refused_before_anything_is_launched(recorder, call, opts, status):
     assert got == status and error and not launches
 
 
-GOOD = [("rotary", dict()), ("rotary", dict(n=1, n_heads=4096, hd=128)), ("rotary", dict(n=1 << 20, rot=2, inter=1)), ("append", dict()), ("append", dict(heads=4, bf16=0)),
+GOOD = [("rotary", dict()), ("rotary", dict(n=1, n_heads=4096, hd=128)), ("rotary", dict(n=1 << 20, rot=2, inter=1)), ("rotary", dict(n=(1 << 25) + 3, n_heads=8, hd=128, rot=2, ld_x=1025, ld_out=1025)), ("rotary", dict(n=2**31 - 1, n_heads=1, hd=64)), ("append", dict()), ("append", dict(heads=4, bf16=0)),
         ("append", dict(n=1 << 22, null="position")), ("append", dict(null="weight")), ("gather", dict(hd=128)), ("gather", dict(heads=4, n=1)), ("attention", dict()),
         ("attention", dict(n_req=65535, max_context=100)), ("attention", dict(n_req=1, max_context=1 << 26, add=1)), ("attention", dict(n_req=2, max_rows=65535, group=8)), ("attention", dict(n_req=1000, max_rows=1048, add=1)),
         ("attention", dict(n_req=1, max_rows=33, max_context=0, hd=128, null="lse")), ("evict", dict()), ("evict", dict(n_req=65535, max_context=10)), ("evict", dict(n_req=1, max_context=1 << 26)),
