@@ -222,3 +222,102 @@ def test_scales_at_four_byte_alignment(torch_mod):
             for count in (1, 5, 60):
                 assert torch.equal(go(s, count), go(s2, count))
             assert torch.equal(moved["weight"].view(torch.uint8), cache.dev["weight"].view(torch.uint8))
+
+
+class Step:
+    """One step of a server on buffers of its own: rotary, append behind the cached tokens, attention with weights, eviction."""
+
+    def __init__(self, torch, B, h, hd, seed, rows, max_rows):
+        self.torch, self.B, self.h, self.max_rows = torch, B, h, max_rows
+        hkv, group, size, mc = 2, 4, 16, 3000
+        gen = torch.Generator().manual_seed(seed)
+        cache = self.cache = R.Cache(B, 600, hkv, size, hd, seed)
+        self.tables_host = [cache.request(mc + max_rows, -(-(mc + max_rows) // size)) for _ in range(3)]
+        self.tables = torch.from_numpy(np.stack(self.tables_host)).cuda()
+        self.s = cache.upload(B)
+        self.start = {n: x.clone() for n, x in cache.dev.items()}
+        self.x = torch.randn((rows, (group + 2) * hkv * hd), generator=gen).to(torch.bfloat16).cuda()
+        self.y = torch.empty((rows, (group + 1) * hkv * hd), dtype=torch.bfloat16, device="cuda")
+        self.freq = torch.from_numpy(B.mace_rotary_frequencies(hd // 2, 1e4, 4.0, 2048)).cuda()
+        self.positions, self.slots = (torch.zeros(rows, dtype=torch.int32, device="cuda") for _ in range(2))
+        self.offsets, self.lens, self.total = (torch.zeros(n, dtype=torch.int32, device="cuda") for n in (4, 3, 3))
+        self.budgets = torch.full((3, hkv), 900, dtype=torch.int32, device="cuda")
+        self.new = torch.empty((3, hkv), dtype=torch.int32, device="cuda")
+        self.out = torch.empty((rows, group * hkv * hd), dtype=torch.bfloat16, device="cuda")
+        self.mc, self.q_cols, self.kv_cols = mc, group * hkv * hd, hkv * hd
+        self.work = torch.empty(B.mace_kv4_attention_workspace_bytes(h, 3, max_rows, mc), dtype=torch.uint8, device="cuda")
+        self.work2 = torch.empty(B.mace_kv4_evict_workspace_bytes(h, 3, mc + max_rows), dtype=torch.uint8, device="cuda")
+
+    def fill(self, lens, counts):
+        torch = self.torch
+        first = np.concatenate([[0], np.cumsum(counts)]).astype(np.int32)
+        positions, slots = np.zeros(len(self.slots), np.int32), np.full(len(self.slots), -1, np.int32)
+        for table, l, c, f in zip(self.tables_host, lens, counts, first):
+            t = l + np.arange(c)
+            positions[f:f + c], slots[f:f + c] = t, table[t // 16] * 16 + t % 16
+        put = lambda to, x: to.copy_(torch.from_numpy(np.asarray(x, dtype=np.int32)))
+        put(self.positions, positions), put(self.slots, slots), put(self.offsets, first), put(self.lens, lens), put(self.total, np.add(lens, counts))
+        for n, x in self.start.items():
+            self.cache.dev[n].copy_(x)
+        self.out.zero_()
+
+    def run(self):
+        B, h = self.B, self.h
+        B.mace_rotary(h, self.x[:, :self.q_cols + self.kv_cols], self.positions, self.freq, self.y, (self.q_cols + self.kv_cols) // self.h.head_dim)
+        B.mace_kv4_append(h, self.s, self.y[:, self.q_cols:], self.x[:, self.q_cols + self.kv_cols:], self.slots, positions=self.positions)
+        B.mace_kv4_attention(h, self.s, self.y[:, :self.q_cols], self.tables, self.lens, self.out, self.work, self.mc, q_offsets=self.offsets, max_rows=self.max_rows, add_weight=True)
+        B.mace_kv4_evict(h, self.s, self.tables, self.total, self.total, self.budgets, self.new, self.work2, self.mc + self.max_rows, 4, 64)
+
+    def result(self):
+        self.torch.cuda.synchronize()
+        return [self.out.clone(), self.new.clone()] + [x.view(self.torch.uint8).clone() for x in self.cache.dev.values()]
+
+
+SIZES = [([900, 20, 2999], [1, 1, 1]), ([0, 2500, 63], [2, 1, 0]), ([3000, 3000, 3000], [2, 2, 2]), ([5, 0, 1], [0, 2, 1])]
+
+
+@pytest.mark.parametrize("hd,max_rows", [(64, 2), (128, 2), (128, 60)])
+def test_a_captured_step_is_replayed_with_other_lengths(torch_mod, hd, max_rows):
+    torch = torch_mod
+    sizes = [(l, [c * max_rows // 2 for c in n]) for l, n in SIZES]
+    with Model(2, hd, True, 4) as (B, h):
+        step, want = Step(torch, B, h, hd, 1, 3 * max_rows, max_rows), []
+        for l, n in sizes:
+            step.fill(l, n)
+            step.run()
+            want.append(step.result())
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.stream(side):
+            with torch.cuda.graph(graph, stream=side):
+                step.run()
+        for turn in range(3):
+            for i in range(len(sizes)):
+                step.fill(*sizes[(i + turn) % len(sizes)])
+                graph.replay()
+                assert all(torch.equal(a, b) for a, b in zip(step.result(), want[(i + turn) % len(sizes)]))
+
+
+def test_two_servers_on_two_streams(torch_mod):
+    """Handles, pools and workspaces of their own: what two streams do at the same time does not meet."""
+    torch = torch_mod
+    with Model(2, 128, True, 4) as (B, h), Model(2, 64, True, 4) as (_, h2):
+        steps = [Step(torch, B, h, 128, 1, 180, 60), Step(torch, B, h2, 64, 2, 6, 2)]
+        sizes = [SIZES[0][0], SIZES[2][0]], [[60, 3, 59], [1, 2, 2]]
+        want = []
+        for step, l, n in zip(steps, *sizes):
+            step.fill(l, n)
+            step.run()
+            want.append(step.result())
+        streams = [torch.cuda.Stream() for _ in steps]
+        for _ in range(5):
+            for step, l, n in zip(steps, *sizes):
+                step.fill(l, n)
+            torch.cuda.synchronize()
+            for step, stream in zip(steps, streams):
+                with torch.cuda.stream(stream):
+                    step.run()
+            torch.cuda.synchronize()
+            for step, w in zip(steps, want):
+                assert all(torch.equal(a, b) for a, b in zip(step.result(), w))
