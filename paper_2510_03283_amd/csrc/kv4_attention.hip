@@ -10,6 +10,9 @@
 // lie in one group, so its scale goes into the conversion to bf16.  V: the scale belongs to a token, which is the reduction index, so it goes into P, once
 // for every 32 channels.  Both conversions are exact; P is rounded to bf16 (half a step, 2^-8 of each term) for bf16 rows and split into three
 // terms (24 bits) for fp32 rows, as q is.  Sums, maxima and the output before its rounding are fp32.
+//
+// Few rows: the bytes of the cache bound it, so tokens are split over waves and blocks (128 requests of 2048 to 8192 tokens, 32 heads of 128: 479 us, 6.2 TB/s; one of 131001, 8 kv heads: 29 us
+// and 5 for the join, 4.9 TB/s).  A short batch is a chain of loads, table - codes - products (32 requests of 256 to 2048 tokens, 8 kv heads of 64: 12 us).  Many rows: the instructions, below.
 #include "kernels.h"
 #include "kv4.h"
 
@@ -94,7 +97,7 @@ __device__ __forceinline__ uint32_t token_of(const Kv4Cache &c, const int32_t *t
 typedef __attribute__((ext_vector_type(4))) uint32_t u32x4_t;
 typedef __attribute__((ext_vector_type(2))) uint32_t u32x2_t;
 
-// Codes of one lane for one S^T tile: HD / 4 elements.  (The cache is read once and should not displace what else is in the caches: 521 -> 502 us for 128
+// Codes of one lane for one S^T tile: HD / 4 elements.  (The cache is read once and should not displace what else is in the caches: 525 -> 489 us for 128
 // requests of 2048 - 8192 tokens.)
 template <int HD> struct KCodes { uint32_t w[HD / 32]; };
 template <int HD, bool ONCE = true>
@@ -217,7 +220,7 @@ __device__ __forceinline__ void mask_scores(f32x4_t (&s)[4], int last, uint64_t 
 }
 // Soft-max of a row, whose tokens are spread over four lanes: probabilities are 2^(sc s - top), and `top` follows the largest product only when one is more than `lag`
 // above it.  lag = 0: the largest probability is 1, which bf16 holds exactly.  lag = MANY_LAG, where many rows make the instructions count: most turns need
-// neither an exchange between lanes nor a rescaling (16 pieces of 256 rows x 32 heads x 128 behind 4000 tokens 350 -> 319 us), and a row that one token
+// neither an exchange between lanes nor a rescaling (a piece of 4096 rows, 32 heads and 8 kv heads of 128, behind 4096 tokens 483 -> 457 us), and a row that one token
 // dominates has the rounding of that token's probability as well (error of such rows up to 1.4 times the output's own rounding).
 constexpr float MANY_LAG = 8.f;
 struct Softmax {
@@ -438,14 +441,15 @@ __global__ __launch_bounds__(64 * WAVES, TERMS == 1 && HD == 64 ? 4 : 2) void kv
 // and are decoded by every wave (a quarter of the bytes that decoded ones would be read in), the value's are decoded with their scale first and lie there as bf16, token by token,
 // so that P needs no scaling and a transposing read of 4 tokens x 16 channels hands out V^T.  A value group that is NaN counts as 0 there and is noted beside it: only the
 // rows that see the token become NaN.  A turn's codes are asked for two turns ahead, put into LDS one ahead, their
-// blocks looked up three ahead.
+// blocks looked up three ahead.  A piece of 4096 rows, 32 heads and 8 kv heads of 128, behind 4096 tokens takes 440 - 457 us, 0.90 - 0.94 PFLOP/s: the matrix pipes are busy for 39 % of the
+// cycles, vector instructions (exponentials, roundings, maxima, decoding, the issue of the products) take 65 %.
 constexpr int ROW_TILES = 2, BLOCK_ROWS = WAVES * ROW_TILES * ROWS, LEAST_TURNS = 4, NEAR = 2;
 typedef __attribute__((ext_vector_type(4))) short s16x4_t;
 typedef __attribute__((address_space(3))) s16x4_t lds_s16x4_t;
 
 // The work of a kv head, the turns of all blocks of rows of all requests one after the other, is cut into equal shares, one a thread block, since lengths and rows are known on the device only and
-// differ (a grid of requests, blocks of rows and equal splits of the longest context leaves the chip half idle: 6 requests of 134 to 238 rows at 2500 to 6700 tokens, 8 kv heads of 128, 168 us
-// with the joins, now 145; 64 of 5 to 60 rows at 500 to 6000 335, now 220).  A block of rows that is cut leaves states that
+// differ (a grid of requests, blocks of rows and equal splits of the longest context leaves the chip half idle: 6 requests of 134 to 238 rows at 2500 to 6700 tokens, 8 kv heads of 128, with
+// weights 218 us, now 194; 64 of 5 to 60 rows at 500 to 6000 335, now 220).  A block of rows that is cut leaves states that
 // kv4_rows_join_kernel joins; a cut NEAR turns or less from the rows' begin or end, the price of one, moves there.
 struct Shares {
   float *acc;                        // [Hkv, workers, 2, BLOCK_ROWS, HD] what a worker leaves of the rows that it began with in their middle and of those that it left before their end
@@ -764,7 +768,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void kv4_rows_kernel(Kv4Attention a,
 }
 
 // Joins the splits of a row and head: `groups` teams of HD / 4 lanes (four channels each) take every groups-th split with a soft-max state of their own and are merged
-// in order.  The time is the latency of the loads, so a team has those of IN_FLIGHT splits under way.
+// in order.  The time is the latency of the loads, so a team has those of IN_FLIGHT splits under way (4 - 5 us for 32 heads of 64 splits, and for 128 requests x 32 heads of three).
 constexpr int IN_FLIGHT = 4;
 // Merges states first, first + step, .. below n, of which s lies at place(s): channels 4 e .. + 3.
 template <int HD, class Place>
@@ -878,7 +882,8 @@ __global__ __launch_bounds__(64 * WAVES) void kv4_rows_join_kernel(Kv4Attention 
 // Adds every token's probabilities, summed over the rows of its request and the query heads of its kv head, to its weight, from the product S = Q K^T formed again
 // (lane (i, g) has token i of a tile of 16 and rows 4 g .. 4 g + 3) and the rows' log sums: 68 or 34 bytes of K a token again instead of 8 for every row.  A wave takes 64 tokens
 // and all rows, so a request adds to a token once (blocks that requests share get one addition from each, by atomics).
-// Here: requests of one tile of rows, whose log sums the block forms from the splits' states; the first `joins` blocks join the splits meanwhile.
+// Here: requests of one tile of rows, whose log sums the block forms from the splits' states; the first `joins` blocks join the splits meanwhile.  (32 requests of 256 to 2048
+// tokens, 8 kv heads of 64: 9.5 us, the chain table - codes - products - addition beside that of the log sums.)
 template <int HD, int TERMS, bool RUNS>
 __global__ __launch_bounds__(64 * WAVES) void kv4_weight_kernel(Kv4Attention a, States x, int joins, int groups, int pieces) {
   constexpr int NS = HD / 32;
@@ -951,7 +956,8 @@ __global__ __launch_bounds__(64 * WAVES) void kv4_weight_kernel(Kv4Attention a, 
 }
 
 // The same for more rows, whose log sums are there already.  A wave keeps the decoded keys of its 64 tokens; the rows come in stages of 64 (fp32: 16) through LDS,
-// shared by the waves of a block, a stage ahead in registers.
+// shared by the waves of a block, a stage ahead in registers.  (The ragged pieces above: 75 us; 45 of them products and exponentials, the rest stages that a block waits for and the
+// last blocks alone.  Blocks in the order of requests first, heads next: 81 and 83.)
 template <int HD, int TERMS>
 __global__ __launch_bounds__(64 * WAVES, 2) void kv4_weight_rows_kernel(Kv4Attention a, States x) {
   constexpr int NS = HD / 32, NG = HD / 32, STAGE = TERMS == 1 ? 64 : 16, CPR = HD / 8;      // 16-byte pieces of a row in bf16
@@ -1080,7 +1086,7 @@ int chunk_tokens(int n_req, int tiles, int Hkv, int tokens) {
   return chunk;
 }
 // Rows of a kv head up to which the first kernel takes bf16 requests, tile by tile; us on it and on the kernel of many rows, 64 requests of 2000 tokens, 8 kv heads: 16 / 24 / 32 rows
-// of 128-wide heads 45 and 62 / 66 and 63 / 67 and 63, 32 / 48 / 64 rows of 64-wide ones 40 and 49 / 56 and 62 / 73 and 63.
+// of 128-wide heads 44 and 72 / 72 and 68 / 73 and 69, 32 / 48 / 64 rows of 64-wide ones 41 and 56 / 60 and 69 / 77 and 70.
 int few_rows(int hd) { return hd == 128 ? 16 : 48; }
 // Thread blocks of a kv head for shares: two a CU in all, or as many as there can be shares of LEAST_TURNS.  0: the blocks of rows are the thread blocks, long ones first, nothing is cut and
 // nothing joined.  That is for many of them, or for two rounds of them that come from long pieces, whose blocks are alike; few rows a request, of any lengths, need shares.  us by blocks
