@@ -133,6 +133,9 @@ __device__ __forceinline__ void move_tokens(const Kv4Cache &c, const Where &w, c
   }
 }
 
+// Bounds of a request's tokens up to which a block moves its own in any case, and moves up to which it does so in longer ones.  (64-wide heads, 8 of each request: 16 requests cut from 8192
+// to 8000 tokens 33 us with a launch for the moves, 21 without, to 4000 41 and 44; 8 of 128-wide heads from 32768 to 32500 46 us with all moves in that launch, 42 with none left for it.)
+constexpr int MOVE_INSIDE = 8192, MOVE_FEW = 512;
 // lists: [n_req, Hkv, 2, most] token numbers: holes, displaced; counts [n_req, Hkv, NWAVES + 1]: of both lists of every wave (as many in all), and the lists' stride.
 template <int HD, bool HELD>
 __global__ __launch_bounds__(THREADS) void kv4_evict_kernel(Kv4Evict a, int most, int32_t *__restrict__ lists, int2 *__restrict__ counts, bool move) {
@@ -259,17 +262,18 @@ __global__ __launch_bounds__(THREADS) void kv4_evict_kernel(Kv4Evict a, int most
     }
   });
   int2 *mine = counts + id * (NWAVES + 1);
-  if (!move) {
-    if (lane == 0) mine[wave] = make_int2(nh, nm);
-    if (tid == 0) mine[NWAVES] = make_int2(64 * per, 0);
-    return;
-  }
   if (lane == 0) { before[wave + 1][0] = nh; before[wave + 1][1] = nm; }
   if (tid < 2) before[0][tid] = 0;
   __syncthreads();                                   // (a block's own global writes are seen by its threads behind a barrier)
   if (tid < 2)
     for (int k = 1; k <= NWAVES; ++k) before[k][tid] += before[k - 1][tid];
   __syncthreads();
+  const bool mine_to_move = move || before[NWAVES][0] <= MOVE_FEW;
+  if (!move) {                                       // what the next launch has to do
+    if (lane == 0) mine[wave] = mine_to_move ? make_int2(0, 0) : make_int2(nh, nm);
+    if (tid == 0) mine[NWAVES] = make_int2(64 * per, 0);
+  }
+  if (!mine_to_move) return;
   move_tokens<HD, 2>(a.c, w, Lists{holes, moved, 64 * per, before}, before[NWAVES][0], tid / LANES<HD>, THREADS / LANES<HD>, tid % LANES<HD>);
 }
 
@@ -298,7 +302,6 @@ __global__ __launch_bounds__(256) void kv4_move_kernel(Kv4Evict a, int most, con
                                  threadIdx.x % LANES<HD>);
 }
 
-constexpr int MOVE_INSIDE = 4096;                   // tokens up to which a block moves its own
 
 // A list has room for all tokens, in whole batches: where a wave's part begins depends on the request's length alone.
 int list_length(int max_context) { return std::max(1, cdiv(max_context, THREADS * BATCH)) * THREADS * BATCH; }

@@ -87,7 +87,8 @@ def test_against_the_definition(torch_mod, weights, hkv, hd, size, lens, budgets
     run(torch_mod, hkv, hd, size, lens, budgets, n_sink, n_recent, weights=weights, seed=sum(lens))
 
 
-@pytest.mark.parametrize("hd,lens,budgets", [(64, [4097, 4096], [2048, 4000]), (128, [9000], [8999]), (64, [32768], [7]), (128, [33000, 500], [20000, 499]), (64, [70001], [35000])])
+@pytest.mark.parametrize("hd,lens,budgets", [(64, [4097, 4096], [2048, 4000]), (128, [9000], [8999]), (64, [32768], [7]), (128, [33000, 500], [20000, 499]), (64, [70001], [35000]),
+                                             (128, [9000, 9000, 8200], [8700, 8000, 8193]), (64, [8193, 100], [7681, 99])])
 def test_long_requests(torch_mod, hd, lens, budgets):
     """Around the lengths where keys no longer fit registers and the moves get a launch of their own."""
     run(torch_mod, 2, hd, 16, lens, budgets, 4, 100, seed=lens[0])
