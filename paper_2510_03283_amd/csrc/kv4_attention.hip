@@ -451,12 +451,13 @@ typedef __attribute__((address_space(3))) s16x4_t lds_s16x4_t;
 // differ (a grid of requests, blocks of rows and equal splits of the longest context leaves the chip half idle: 6 requests of 134 to 238 rows at 2500 to 6700 tokens, 8 kv heads of 128, with
 // weights 218 us, now 194; 64 of 5 to 60 rows at 500 to 6000 335, now 220).  A block of rows that is cut leaves states that
 // kv4_rows_join_kernel joins; a cut NEAR turns or less from the rows' begin or end, the price of one, moves there.
+// (With workers = 0 the thread blocks are the splits of the blocks of rows, as few rows have them.)
 struct Shares {
   float *acc;                        // [Hkv, workers, 2, BLOCK_ROWS, HD] what a worker leaves of the rows that it began with in their middle and of those that it left before their end
   float2 *ml;                        // [Hkv, workers, 2, BLOCK_ROWS]
   float *lse2;
   int4 *start;                       // [Hkv, workers] request, block of rows, turn in it (0: nothing cut)
-  int workers;
+  int workers, nsplit, chunk;        // chunk: turns of a split
 };
 // Turns of the blocks of rows of a request.  (Rows that see nothing have some as well: they are written.)
 struct Turns {
@@ -561,7 +562,9 @@ __global__ __launch_bounds__(64 * WAVES, 2) void kv4_rows_kernel(Kv4Attention a,
     tile = gridDim.x / a.c.Hkv - 1 - worker;           // long ones first
     const Rows w = rows_of<BLOCK_ROWS>(a, req, kvh, tile);
     if (w.m0 >= w.m1) return;
-    left = Turns(a, w).of(tile);
+    turn0 = blockIdx.z * x.chunk;
+    left = min(x.chunk, Turns(a, w).of(tile) - turn0);
+    if (left <= 0) return;
   }
 
   for (;; ++tile, turn0 = 0) {
@@ -572,7 +575,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void kv4_rows_kernel(Kv4Attention a,
     w = rows_of<BLOCK_ROWS>(a, req, kvh, 0);
   }
   const int turns = Turns(a, w).of(tile), turn1 = min(turns, turn0 + left);
-  const bool cut = turn0 > 0 || turn1 < turns;
+  const bool cut = x.workers > 0 ? turn0 > 0 || turn1 < turns : x.nsplit > 1;
   const int c0 = turn0 * TURN, c1 = min(w.ctx + query_of(a, w.m1 - 1) + 1, turn1 * TURN);
   const int32_t *table = a.tables + (size_t)w.req * a.max_blocks;
   __syncthreads();                                     // nobody reads the rows before any more
@@ -755,7 +758,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void kv4_rows_kernel(Kv4Attention a,
         if (a.add_weight) x.lse2[at] = lse2;
       }
     } else {
-      const size_t state = (((size_t)kvh * x.workers + worker) * 2 + (turn0 == 0)) * BLOCK_ROWS + (mr - w.m0);
+      const size_t state = x.workers > 0 ? (((size_t)kvh * x.workers + worker) * 2 + (turn0 == 0)) * BLOCK_ROWS + (mr - w.m0) : at * x.nsplit + blockIdx.z;
       float *to = x.acc + state * HD + 4 * g;
 #pragma unroll
       for (int c = 0; c < CT; ++c) *(f32x4_t *)(to + 16 * c) = o[b][c];
@@ -1088,22 +1091,29 @@ int chunk_tokens(int n_req, int tiles, int Hkv, int tokens) {
 // Rows of a kv head up to which the first kernel takes bf16 requests, tile by tile; us on it and on the kernel of many rows, 64 requests of 2000 tokens, 8 kv heads: 16 / 24 / 32 rows
 // of 128-wide heads 44 and 72 / 72 and 68 / 73 and 69, 32 / 48 / 64 rows of 64-wide ones 41 and 56 / 60 and 69 / 77 and 70.
 int few_rows(int hd) { return hd == 128 ? 16 : 48; }
-// Thread blocks of a kv head for shares: two a CU in all, or as many as there can be shares of LEAST_TURNS.  0: the blocks of rows are the thread blocks, long ones first, nothing is cut and
-// nothing joined.  That is for many of them, or for two rounds of them that come from long pieces, whose blocks are alike; few rows a request, of any lengths, need shares.  us by blocks
-// and by shares, 8 kv heads of 128: a piece of 4096 rows behind 4096 tokens 439 and 483, three of 600 to 2000 rows 135 and 159; 96 requests of 5 to 60 rows at 500 to 6000 tokens 488 and 340,
-// 120 of them 561 and 407 (16 of 256 rows at 4000 each, 32 heads: 377 and 398).
-constexpr int ENOUGH = 2000, ENOUGH_ALIKE = 1024, ALIKE = 16;
+// Splits of a block of rows: two thread blocks a CU, or splits of four turns.
+int rows_chunk(int n_req, int tiles, int Hkv, int tokens) {
+  const long long blocks = (long long)n_req * Hkv * tiles;
+  const int nsplit = (int)std::max(1ll, std::min<long long>(cdiv(tokens, 4 * TURN), (512 + blocks - 1) / blocks));
+  return cdiv(cdiv(tokens, nsplit), TURN) * TURN;
+}
+// Thread blocks of a kv head for shares, two a CU in all; 0: blocks of rows and their splits are the thread blocks, long ones first.  That is for many blocks of rows, for twice as many as run at once
+// that come from long pieces, whose blocks are alike, and for short work, where finding the shares costs more than they give; few rows a request, of any lengths, need shares.  us by
+// blocks and by shares, 8 kv heads of 128: a piece of 4096 rows behind 4096 tokens 439 and 483, three of 600 to 2000 rows 135 and 159; 96 requests of 5 to 60 rows at 500 to 6000 tokens 488
+// and 340, 120 of them 561 and 407 (16 of 256 rows at 4000 each, 32 heads: 377 and 398); one of 64 rows at 2000 22 and 34, 64 of 8 rows at 300 to 700 28 and 38, 32 of 5 to 30 rows
+// at 300 to 2000, 16 turns a share, 55 and 48, six of 37 to 256 rows at 1000 to 2000, 24 turns, 77 and 62.
+constexpr int ENOUGH = 2000, ENOUGH_ALIKE = 1024, ALIKE = 16, SHORT = 14;
 int workers_of(int n_req, int tiles, int Hkv, int tokens) {
   const long long blocks = (long long)n_req * tiles, turns = blocks * cdiv(tokens, TURN);
-  if (blocks * Hkv >= (tiles >= ALIKE ? ENOUGH_ALIKE : ENOUGH)) return 0;
-  return (int)std::max(1ll, std::min<long long>(512 / Hkv, (turns + LEAST_TURNS - 1) / LEAST_TURNS));
+  const int workers = std::max(1, 512 / Hkv);
+  return blocks * Hkv >= (tiles >= ALIKE ? ENOUGH_ALIKE : ENOUGH) || turns < (long long)SHORT * workers ? 0 : workers;
 }
 static_assert(ENOUGH * (((1ll << 26) + 65535) / TURN + 1) < INT32_MAX, "turns of a kv head");
 // Copies of a row in a tile: as many as rows and scale groups leave room for.
 int copies(int rows, int hd) { return rows <= 4 && hd == 128 ? 4 : rows <= 8 ? 2 : 1; }
 
 struct Plan {
-  bool many;                 // blocks of many rows, by `workers` a kv head
+  bool many;                 // blocks of many rows, by `workers` a kv head where that is not 0
   int rep, tile_rows, tiles, nsplit, chunk, workers;
   size_t rows;
 };
@@ -1114,24 +1124,24 @@ Plan plan_of(int n_req, int max_rows, int max_context, int Hq, int Hkv, int hd, 
   p.rep = copies(rows, hd);
   p.tile_rows = p.many ? BLOCK_ROWS : ROWS / p.rep;
   p.tiles = cdiv(rows, p.tile_rows);
-  p.workers = workers_of(n_req, p.tiles, Hkv, tokens);
-  p.chunk = chunk_tokens(n_req, p.tiles, Hkv, tokens);
+  p.workers = p.many ? workers_of(n_req, p.tiles, Hkv, tokens) : 0;
+  p.chunk = p.workers ? tokens : p.many ? rows_chunk(n_req, p.tiles, Hkv, tokens) : chunk_tokens(n_req, p.tiles, Hkv, tokens);
   p.nsplit = cdiv(tokens, p.chunk);
   p.rows = (size_t)n_req * max_rows * Hq;
   return p;
 }
-// A workspace: log sums of all rows, states of few rows (acc for several splits only) or shares and what they leave.
+// A workspace: log sums of all rows, states of the splits (acc for several only) or shares and what they leave.
 struct Layout {
   size_t lse2, ml, start, acc, bytes;
 };
 Layout layout_of(const Plan &p, int Hkv, int hd) {
   Layout l;
-  const size_t states = p.many ? (size_t)Hkv * p.workers * 2 * BLOCK_ROWS : p.rows * p.nsplit;
+  const size_t states = p.workers ? (size_t)Hkv * p.workers * 2 * BLOCK_ROWS : p.rows * p.nsplit;
   l.lse2 = 0;
   l.ml = align_up(p.rows * sizeof(float), 256);
   l.start = l.ml + align_up(states * sizeof(float2), 256);
-  l.acc = l.start + (p.many ? align_up((size_t)Hkv * p.workers * sizeof(int4), 256) : 0);
-  l.bytes = l.acc + (p.many || p.nsplit > 1 ? states * hd * sizeof(float) : 0);
+  l.acc = l.start + (p.workers ? align_up((size_t)Hkv * p.workers * sizeof(int4), 256) : 0);
+  l.bytes = l.acc + (p.workers || p.nsplit > 1 ? states * hd * sizeof(float) : 0);
   return l;
 }
 
@@ -1149,15 +1159,15 @@ hipError_t launch_kv4_attention(const Kv4Attention &a, bool bf16, void *scratch,
   char *at = (char *)scratch;
   const Layout l = layout_of(p, Hkv, hd);
   const States x = {(float *)(at + l.acc), (float2 *)(at + l.ml), (float *)(at + l.lse2), p.nsplit, p.chunk, p.tile_rows};
-  const Shares shares = {(float *)(at + l.acc), (float2 *)(at + l.ml), (float *)(at + l.lse2), (int4 *)(at + l.start), p.workers};
+  const Shares shares = {(float *)(at + l.acc), (float2 *)(at + l.ml), (float *)(at + l.lse2), (int4 *)(at + l.start), p.workers, p.nsplit, cdiv(p.chunk, TURN)};
   auto main = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(Hkv * p.tiles, p.nsplit, a.n_req), dim3(64 * WAVES), 0, st, a, x, p.tiles); };
   auto many = [&](auto kernel, auto join) {
-    hipLaunchKernelGGL(kernel, p.workers ? dim3(Hkv * p.workers) : dim3(Hkv * p.tiles, a.n_req), dim3(64 * WAVES), 0, st, a, shares);
+    hipLaunchKernelGGL(kernel, p.workers ? dim3(Hkv * p.workers) : dim3(Hkv * p.tiles, a.n_req, p.nsplit), dim3(64 * WAVES), 0, st, a, shares);
     if (p.workers > 1) hipLaunchKernelGGL(join, dim3(p.workers - 1, Hkv, BLOCK_ROWS * (hd / 4) / (64 * WAVES)), dim3(64 * WAVES), 0, st, a, shares);
   };
   // teams of a row and head: one up to the splits that it has under way at once, else four or all of a block
   const int teams = 64 * WAVES / (hd / 4), groups = p.nsplit <= IN_FLIGHT ? 1 : p.nsplit <= 4 * IN_FLIGHT ? 4 : teams;
-  const int joins = !p.many && p.nsplit > 1 ? (int)((p.rows * groups + teams - 1) / teams) : 0, pieces = cdiv(tokens, TURN * WAVES);
+  const int joins = p.nsplit > 1 ? (int)((p.rows * groups + teams - 1) / teams) : 0, pieces = cdiv(tokens, TURN * WAVES);
   const bool one_tile = a.max_rows * a.group <= ROWS;
   auto join = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(joins), dim3(64 * WAVES), 0, st, a, x, groups); };
   auto weight = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(joins + Hkv * pieces * a.n_req), dim3(64 * WAVES), 0, st, a, x, joins, groups, pieces); };

@@ -49,7 +49,7 @@ def check(torch, bf16, cache, tables, lens, rows, q, out, lse, before, scale, we
             assert (np.abs(now - expect) <= slack)[~np.isnan(expect)].all(), np.nanmax(np.abs(now - expect) / slack)
 
 
-def run(torch, bf16, hkv, group, hd, size, lens, counts, offsets=True, per_head=False, gap=0, scale=None, wide=False, spread=1.0, seed=0, add_weight=True, extra=0, ld=0, most=1):
+def run(torch, bf16, hkv, group, hd, size, lens, counts, offsets=True, per_head=False, gap=0, scale=None, wide=False, spread=1.0, seed=0, add_weight=True, extra=0, ld=0, most=1, bound=0):
     """One call: requests of lens[r] cached tokens and counts[r] new rows; `gap` rows in front and behind that belong to nobody."""
     r = np.random.default_rng(seed)
     dtype = torch.bfloat16 if bf16 else torch.float32
@@ -69,7 +69,7 @@ def run(torch, bf16, hkv, group, hd, size, lens, counts, offsets=True, per_head=
         d_lens = torch.tensor(heads if per_head else lens, dtype=torch.int32, device="cuda")
         d_off = torch.from_numpy(first.astype(np.int32)).cuda() if offsets else None
         d_tab = torch.from_numpy(np.stack(tables)).cuda()
-        mc, mr = max(lens), max(counts + [most])
+        mc, mr = max(lens + [bound]), max(counts + [most])
         sizes = (len(lens), mr, mc)
         B.mace_kv4_attention(h, s, q.cuda(), d_tab, d_lens, out, workspace(torch, B, h, *sizes), mc, q_offsets=d_off, max_rows=mr, lse=lse, scale=scale, add_weight=add_weight)
         torch.cuda.synchronize()
@@ -98,11 +98,13 @@ def test_several_rows_a_request(torch_mod, bf16, hkv, group, hd, size, lens, cou
 
 
 @pytest.mark.parametrize("hkv,group,hd,lens,counts,per_head", [
-    (1, 8, 128, [5000], [16], False), (1, 4, 64, [9000, 3], [15, 40], False),             # rows that many thread blocks work on
+    (1, 8, 128, [5000], [17], False), (1, 4, 64, [9000, 3], [15, 40], False),             # rows that many thread blocks work on
     (2, 4, 128, [0, 700, 64, 1300, 5, 0, 2000], [33, 5, 0, 200, 1, 0, 70], True), (3, 1, 128, [300, 0, 100], [130, 260, 1], True),
     (1, 2, 64, [63, 64, 65, 127, 128, 129], [64, 64, 64, 65, 63, 128], False)])
-def test_rows_cut_into_shares(torch_mod, hkv, group, hd, lens, counts, per_head):
-    run(torch_mod, True, hkv, group, hd, 16, lens, counts, per_head=per_head, gap=1, seed=sum(lens))
+@pytest.mark.parametrize("shares", [True, False])
+def test_rows_cut_into_shares(torch_mod, hkv, group, hd, lens, counts, per_head, shares):
+    """Shares where the bounds promise work enough, else equal splits of blocks of rows."""
+    run(torch_mod, True, hkv, group, hd, 16, lens, counts, per_head=per_head, gap=1, seed=sum(lens), bound=64 * 24 * 512 if shares else 0)
 
 
 @pytest.mark.parametrize("hd", [64, 128])
@@ -110,7 +112,7 @@ def test_more_requests_than_threads(torch_mod, hd):
     r = np.random.default_rng(hd)
     lens, counts = [int(x) for x in r.integers(0, 60, 600)], [int(x) for x in r.integers(0, 4, 600)]
     counts[17], lens[400] = 60, 900
-    run(torch_mod, True, 1, 2, hd, 16, lens, counts, seed=1)
+    run(torch_mod, True, 1, 2, hd, 16, lens, counts, seed=1, bound=4000)
 
 
 @pytest.mark.parametrize("hd", [64, 128])

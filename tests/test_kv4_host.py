@@ -133,7 +133,7 @@ def test_every_kernel_is_reached(recorder):
     assert launched(recorder, "rotary", rot) == built_kernels("rotary")
     both = [dict(bf16=b, hd=d) for b in (0, 1) for d in (64, 128)]
     assert launched(recorder, "append", both) | launched(recorder, "gather", both) == built_kernels("kv4_cache")
-    sizes = [dict(n_req=q, max_rows=r, max_context=c, group=g, add=w, block=s) for w in (0, 1) for q, r, c in ((1, 1, 100), (3, 1, 100000), (5, 3, 500), (4, 40, 300), (64, 1, 4000), (2, 300, 5000)) for g in (1, 2, 4, 8) for s in (1, 16)]
+    sizes = [dict(n_req=q, max_rows=r, max_context=c, group=g, add=w, block=s) for w in (0, 1) for q, r, c in ((1, 1, 100), (3, 1, 100000), (5, 3, 500), (4, 40, 300), (64, 1, 4000), (2, 300, 5000), (40, 20, 9000)) for g in (1, 2, 4, 8) for s in (1, 16)]
     assert launched(recorder, "attention", [{**s, **b} for s in sizes for b in both]) == built_kernels("kv4_attention")
     assert launched(recorder, "evict", [dict(hd=d, max_context=c) for d in (64, 128) for c in (100, 3000, 5000, 20000, 40000)]) == built_kernels("kv4_evict")
 
