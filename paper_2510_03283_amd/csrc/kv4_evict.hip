@@ -303,8 +303,8 @@ __global__ __launch_bounds__(256) void kv4_move_kernel(Kv4Evict a, int most, con
 }
 
 
-// A list has room for all tokens, in whole batches: where a wave's part begins depends on the request's length alone.
-int list_length(int max_context) { return std::max(1, cdiv(max_context, THREADS * BATCH)) * THREADS * BATCH; }
+// Entries of a list: none lies behind the token that it names.
+int list_length(int max_context) { return std::max(64, (max_context + 63) / 64 * 64); }
 size_t counts_bytes(int n_req, int Hkv) { return align_up((size_t)n_req * Hkv * (NWAVES + 1) * sizeof(int2), 256); }
 
 }  // namespace

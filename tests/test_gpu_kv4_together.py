@@ -191,6 +191,33 @@ def test_nothing_behind_the_workspace_is_written(torch_mod, max_rows, group, bf1
             assert all(torch.equal(a.view(torch.uint8) if a.dtype != torch.int32 else a, b.view(torch.uint8) if b.dtype != torch.int32 else b) for a, b in zip(results[0], other))
 
 
+@pytest.mark.parametrize("mc", [1, 63, 64, 65, 1000, 8193])
+def test_lists_of_the_eviction_fit_their_workspace(torch_mod, mc):
+    """Every token of the first half goes, every one behind it stays: the longest lists that there are."""
+    torch = torch_mod
+    hkv, hd, size = 2, 64, 16
+    with Model(hkv, hd, True) as (B, h):
+        cache = R.Cache(B, 2 * (mc // size + 1), hkv, size, hd, 3)
+        table = np.stack([cache.request(mc, mc // size + 1) for _ in range(2)])
+        t = np.arange(mc)
+        for r in range(2):
+            for hh in range(hkv):
+                cache.weight[table[r][t // size], hh, t % size] = t
+        s = cache.upload(B)
+        i32 = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")
+        need = B.mace_kv4_evict_workspace_bytes(h, 2, mc)
+        work = torch.full((need + 4096,), 0xAB, dtype=torch.uint8, device="cuda")
+        new = torch.empty((2, hkv), dtype=torch.int32, device="cuda")
+        keep = (mc + 1) // 2
+        B.mace_kv4_evict(h, s, torch.from_numpy(table).cuda(), i32([mc, mc]), i32([mc, mc]), i32([[keep] * hkv] * 2), new, work[:need], mc)
+        torch.cuda.synchronize()
+        assert (work[need:] == 0xAB).all() and (new == keep).all()
+        got = cache.dev["weight"].cpu().numpy()
+        for r in range(2):
+            for hh in range(hkv):
+                assert sorted(got[table[r][t // size], hh, t % size][:keep]) == list(range(mc - keep, mc))
+
+
 def test_scales_at_four_byte_alignment(torch_mod):
     """k_scale, v_scale, weight and position may begin at any multiple of four bytes."""
     torch = torch_mod
