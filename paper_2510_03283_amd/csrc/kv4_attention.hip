@@ -771,7 +771,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void kv4_rows_kernel(Kv4Attention a,
 }
 
 // Joins the splits of a row and head: `groups` teams of HD / 4 lanes (four channels each) take every groups-th split with a soft-max state of their own and are merged
-// in order.  The time is the latency of the loads, so a team has those of IN_FLIGHT splits under way (4 - 5 us for 32 heads of 64 splits, and for 128 requests x 32 heads of three).
+// in order.  The time is the latency of the loads, so a team has those of IN_FLIGHT splits under way (4 us for 32 heads of 64 splits).
 constexpr int IN_FLIGHT = 4;
 // Merges states first, first + step, .. below n, of which s lies at place(s): channels 4 e .. + 3.
 template <int HD, class Place>
@@ -1081,11 +1081,16 @@ __global__ __launch_bounds__(64 * WAVES, 2) void kv4_weight_rows_kernel(Kv4Atten
 
 // Tokens of a block: 4096, less where that makes fewer blocks than two a CU, not below four turns of its waves (a second launch to join splits costs
 // more than it saves below that).  us at 256 / 512 / 1024 / 2048 / 4096 tokens, one row a request, 4 query heads a kv head: 4 requests of 400 - 1000 tokens, 8 kv heads of 128
-// 15.4 / 12.5 / 11.2 / 12.0 / 11.1; 16 of 1500 - 4000 22.5 / 22.1 / 19.9 / 22.3 / 26.9; 64 of 1500 - 4000 61 / 55 / 52 / 52 / 43; 1 of 60000 29.2 / 23.8 / 22.7 / 23.7 / 31.6;
-// 256 of 8000 - 16000 863 / 751 / 686 / 654 / 627.
+// 15.4 / 12.5 / 11.2 / 12.0 / 11.1; 16 of 1500 - 4000 22.5 / 22.1 / 19.9 / 22.3 / 26.9; 64 of 1500 - 4000 61 / 55 / 52 / 52 / 43; 1 of 60000 29.2 / 23.8 / 22.7 / 23.7 / 31.6.
+// Requests of up to 16384 tokens are not split where there are six blocks a CU without that, since a block's first loads and its end are worth two turns: at 4096 and whole 256 of 4000 - 16000 581 and
+// 496, 192 of them with 64-wide heads 288 and 255, 1024 2257 and 1762 (1024 blocks, 32 requests of 32 kv heads: 224 and 240; 300 of 1000 - 60000: 1667, and 2125 at 16384, where the last
+// long ones are alone).  More than 65536 blocks are never wanted, nor more than 16384 where a request has several tiles (one piece of 4096 fp32 rows at 16000: 4800 and 4400), so that the
+// states of splits take no more than 540 MB.
 int chunk_tokens(int n_req, int tiles, int Hkv, int tokens) {
-  int chunk = 4096;
-  while (chunk > 4 * WAVES * TURN && (long long)n_req * Hkv * tiles * cdiv(tokens, chunk) < 512) chunk /= 2;
+  const long long blocks = (long long)n_req * Hkv * tiles;
+  int chunk = blocks >= 1536 && tokens <= 16384 ? 16384 : 4096;
+  while (chunk > 4 * WAVES * TURN && blocks * cdiv(tokens, chunk) < 512) chunk /= 2;
+  while (chunk < tokens && blocks * cdiv(tokens, chunk) > (tiles > 1 ? 16384 : 65536)) chunk *= 2;
   return chunk;
 }
 // Rows of a kv head up to which the first kernel takes bf16 requests, tile by tile; us on it and on the kernel of many rows, 64 requests of 2000 tokens, 8 kv heads: 16 / 24 / 32 rows

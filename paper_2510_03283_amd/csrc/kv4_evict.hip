@@ -302,7 +302,6 @@ __global__ __launch_bounds__(256) void kv4_move_kernel(Kv4Evict a, int most, con
                                  threadIdx.x % LANES<HD>);
 }
 
-
 // Entries of a list: none lies behind the token that it names.
 int list_length(int max_context) { return std::max(64, (max_context + 63) / 64 * 64); }
 size_t counts_bytes(int n_req, int Hkv) { return align_up((size_t)n_req * Hkv * (NWAVES + 1) * sizeof(int2), 256); }
