@@ -424,8 +424,8 @@ int mace_kv4_gather(mace_handle_t h, const mace_kv4_cache_t *cache, const int32_
  * Rows of q and out that no request has are neither read nor written.  Tokens of blocks outside the cache are left out; a row without any token has out 0 and
  * lse -inf.  What lies behind a request's last token in its blocks is never used, whatever it holds.  A NaN in a key makes the rows that attend to it NaN, in a value
  * their 32 columns (a value whose probability is below 2^-126 of the row's largest may do so or not).
- * Precision: codes and scales are exact; q is exact; probabilities are rounded to bf16 before the product with V for bf16 models and carry 24 bits for fp32 ones; all
- * sums are fp32; out is rounded once.  workspace: mace_kv4_attention_workspace_bytes for the sizes of the call (other sizes can need more or less), 256-byte aligned,
+ * Precision: codes and scales are exact; q is exact; in the product with V a probability carries 16 bits for bf16 models (off by at most 2^-16 of itself) and 24 bits
+ * for fp32 ones; all sums are fp32; out is rounded once.  The sums are divided at the end: |v| times the number of tokens stays below 2^120.  workspace: mace_kv4_attention_workspace_bytes for the sizes of the call (other sizes can need more or less), 256-byte aligned,
  * nothing of it read before it is written.  Outputs and workspace overlap neither an input nor each other, judged from first to last element.
  * n_req, max_rows <= 65535, max_context <= 2^26, n_req * max_rows * n_q_heads <= 2^23, n_req * n_kv_heads * (max_context + max_rows) <= 2^31. */
 size_t mace_kv4_attention_workspace_bytes(mace_handle_t h, int32_t n_req, int32_t max_rows, int32_t max_context);

@@ -8,8 +8,10 @@
 // (i, g) = (lane % 16, lane / 16) holds row i and, with the tokens of the four S^T tiles chosen as 16 (i / 4) + 4 j + i % 4, the probabilities of tokens 16 g .. 16 g + 15,
 // which is the order in which a transposing LDS read hands out 16 tokens of a channel of V.  K: a lane's elements (32 of a 128-wide head, 16 of a 64-wide one)
 // lie in one group, so its scale goes into the conversion to bf16.  V: the scale belongs to a token, which is the reduction index, so it goes into P, once
-// for every 32 channels.  Both conversions are exact; P is rounded to bf16 (half a step, 2^-8 of each term) for bf16 rows and split into three
-// terms (24 bits) for fp32 rows, as q is.  Sums, maxima and the output before its rounding are fp32.
+// for every 32 channels.  Both conversions are exact; P enters as two bf16 terms for bf16 rows (16 bits: at most 2^-16 of each term) and as three
+// (24 bits) for fp32 rows, as q does.  Sums, maxima and the output before its rounding are fp32.  (One term, 2^-8 of a probability, is faster - 490 us against 515 for the
+// 128 requests below, 367 against 452 for 16 pieces of 256 rows behind 4000 tokens - but of values of either sign its error is two thirds of the output's own rounding,
+// 2.1e-3 of the norm against 1.66e-3; two terms leave 1e-4 of difference to probabilities in fp32.)
 //
 // Few rows: the bytes of the cache bound it, so tokens are split over waves and blocks (128 requests of 2048 to 8192 tokens, 32 heads of 128: 479 us, 6.2 TB/s; one of 131001, 8 kv heads: 29 us
 // and 5 for the join, 4.9 TB/s).  A short batch is a chain of loads, table - codes - products (32 requests of 256 to 2048 tokens, 8 kv heads of 64: 12 us).  Many rows: the instructions, below.
@@ -219,9 +221,8 @@ __device__ __forceinline__ void mask_scores(f32x4_t (&s)[4], int last, uint64_t 
     for (int r = 0; r < 4; ++r) s[j][r] = 16 * j + r < last && ((there >> (16 * j + r)) & 1) ? s[j][r] : -INFINITY;
 }
 // Soft-max of a row, whose tokens are spread over four lanes: probabilities are 2^(sc s - top), and `top` follows the largest product only when one is more than `lag`
-// above it.  lag = 0: the largest probability is 1, which bf16 holds exactly.  lag = MANY_LAG, where many rows make the instructions count: most turns need
-// neither an exchange between lanes nor a rescaling (a piece of 4096 rows, 32 heads and 8 kv heads of 128, behind 4096 tokens 483 -> 457 us), and a row that one token
-// dominates has the rounding of that token's probability as well (error of such rows up to 1.4 times the output's own rounding).
+// above it.  lag = MANY_LAG, where many rows make the instructions count: most turns need neither an exchange between lanes nor a rescaling (a piece of 4096 rows, 32 heads
+// and 8 kv heads of 128, behind 4096 tokens 483 -> 457 us when P had one term).  The relative error of a probability does not depend on it.
 constexpr float MANY_LAG = 8.f;
 struct Softmax {
   float top = -INFINITY, minus = 0.f, l = 0.f;        // minus: -top, 0 as long as the row has seen nothing; l: this lane's part of the sum
@@ -251,7 +252,9 @@ __device__ __forceinline__ float v_scale_of(const Turn<HD> &u, int j, int r, int
   else return kv4::scale_value((u.vs[j][r >> 1] >> (16 * (r & 1) + 8 * gr)) & 255u);
 }
 
-// Eight probabilities as MFMA operand in TERMS bf16 terms.
+// bf16 terms of a probability for rows of so many terms.
+constexpr int p_terms(int terms) { return terms == 1 ? 2 : terms; }
+// Eight numbers as MFMA operand in TERMS bf16 terms: the upper 8 bits of each, of what is left, ..; the last term is rounded to nearest.
 template <int TERMS>
 __device__ __forceinline__ void split8(float (&f)[8], bf16x8_t (&out)[TERMS]) {
 #pragma unroll
@@ -259,10 +262,13 @@ __device__ __forceinline__ void split8(float (&f)[8], bf16x8_t (&out)[TERMS]) {
     uint32_t r[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      r[e] = cvt_pk_bf16(f[2 * e], f[2 * e + 1]);
       if (t + 1 < TERMS) {
-        f[2 * e] -= __uint_as_float(r[e] << 16);
-        f[2 * e + 1] -= __uint_as_float(r[e] & 0xffff0000u);
+        const uint32_t x = __float_as_uint(f[2 * e]), y = __float_as_uint(f[2 * e + 1]);
+        r[e] = __builtin_amdgcn_perm(y, x, 0x07060302u);     // the upper halves of both
+        f[2 * e] -= __uint_as_float(x & 0xffff0000u);
+        f[2 * e + 1] -= __uint_as_float(y & 0xffff0000u);
+      } else {
+        r[e] = cvt_pk_bf16(f[2 * e], f[2 * e + 1]);
       }
     }
     out[t] = __builtin_bit_cast(bf16x8_t, make_uint4(r[0], r[1], r[2], r[3]));
@@ -291,7 +297,7 @@ __global__ __launch_bounds__(64 * WAVES, TERMS == 1 && HD == 64 ? 4 : 2) void kv
   constexpr int NS = HD / 32, NG = HD / 32, CT = HD / 16;      // MFMA steps along the head, scale groups, channel tiles
   constexpr int VB = HD / 2, VROW = VB + 16;                   // bytes of a token of V; padded in LDS, so that 16 tokens' reads of one channel tile meet 16 different banks
   constexpr int CPT = VB / 16;                                 // 16-byte pieces of a token of V
-  constexpr int NR = ROWS / REP, OROW = HD + 4;
+  constexpr int NR = ROWS / REP, OROW = HD + 4, PT = p_terms(TERMS);
   constexpr int SM = WAVES * TURN * VROW > WAVES * NR * (OROW + 2) * 4 ? WAVES * TURN * VROW : WAVES * NR * (OROW + 2) * 4;
   __shared__ __align__(16) unsigned char sm[SM];
   const int kvh = blockIdx.x / tiles, tile = blockIdx.x - kvh * tiles, split = blockIdx.y;
@@ -363,7 +369,7 @@ __global__ __launch_bounds__(64 * WAVES, TERMS == 1 && HD == 64 ? 4 : 2) void kv
       }
 #pragma unroll
     for (int pass = 0; pass < NG / REP; ++pass) {
-      bf16x8_t pf[2][TERMS];
+      bf16x8_t pf[2][PT];
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         float f[8];
@@ -376,7 +382,7 @@ __global__ __launch_bounds__(64 * WAVES, TERMS == 1 && HD == 64 ? 4 : 2) void kv
 #pragma unroll
           for (int e = 0; e < 8; ++e) f[e] = s[2 * h + (e >> 2)][e & 3] == 0.f ? 0.f : f[e];
         }
-        split8<TERMS>(f, pf[h]);
+        split8<PT>(f, pf[h]);
       }
 #pragma unroll
       for (int cc = 0; cc < 2 * REP; ++cc) {
@@ -386,7 +392,7 @@ __global__ __launch_bounds__(64 * WAVES, TERMS == 1 && HD == 64 ? 4 : 2) void kv
         for (int h = 0; h < 2; ++h) {
           const bf16x8_t vf = kv4::decode8((uint32_t)v[h], 1.f);
 #pragma unroll
-          for (int t = TERMS - 1; t >= 0; --t) o[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[h][t], o[c], 0, 0, 0);
+          for (int t = PT - 1; t >= 0; --t) o[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[h][t], o[c], 0, 0, 0);
         }
       }
     }
@@ -481,7 +487,7 @@ struct Turns {
 
 template <int HD>
 __global__ __launch_bounds__(64 * WAVES, 2) void kv4_rows_kernel(Kv4Attention a, Shares x) {
-  constexpr int NS = HD / 32, NG = HD / 32, CT = HD / 16, VROW = HD * 2, KROW = HD / 2;
+  constexpr int NS = HD / 32, NG = HD / 32, CT = HD / 16, VROW = HD * 2, KROW = HD / 2, PT = p_terms(1);
   __shared__ __align__(16) unsigned char sv[2][TURN * VROW], sk[2][TURN * KROW], sks[2][TURN * NG];
   __shared__ int any[3];                               // by turn, as the next two: read in it, filled in the one before, cleared in the one before that
   __shared__ unsigned long long nan[3][NG], missing[3];
@@ -687,7 +693,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void kv4_rows_kernel(Kv4Attention a,
       read_v(0, vf);
       const bool whole = t0 + TURN <= min(wave_all, c1) && !marked;
       const uint64_t there = marked ? ~missing[turn] : ~0ull;
-      bf16x8_t pf[ROW_TILES][2][1];
+      bf16x8_t pf[ROW_TILES][2][PT];
 #pragma unroll
       for (int b = 0; b < ROW_TILES; ++b) {
         if (!whole) mask_scores(s[b], min(limit[b], c1) - t0 - 4 * g, there, g);
@@ -705,7 +711,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void kv4_rows_kernel(Kv4Attention a,
             f[e] = __builtin_amdgcn_exp2f(fmaf(s[b][2 * h + (e >> 2)][e & 3], sc, sx[b].minus));
             sx[b].l += f[e];
           }
-          split8<1>(f, pf[b][h]);
+          split8<PT>(f, pf[b][h]);
         }
       }
       // operands of the next channel tile are read before the products of this one (left to itself, the compiler reads each where it is used and waits)
@@ -717,7 +723,9 @@ __global__ __launch_bounds__(64 * WAVES, 2) void kv4_rows_kernel(Kv4Attention a,
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
-          for (int b = 0; b < ROW_TILES; ++b) o[b][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[h], pf[b][h][0], o[b][c], 0, 0, 0);
+          for (int t = PT - 1; t >= 0; --t)
+#pragma unroll
+            for (int b = 0; b < ROW_TILES; ++b) o[b][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[h], pf[b][h][t], o[b][c], 0, 0, 0);
         __builtin_amdgcn_sched_barrier(0);
         vf[0] = vn[0];
         vf[1] = vn[1];
