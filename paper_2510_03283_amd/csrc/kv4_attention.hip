@@ -1056,18 +1056,18 @@ __global__ __launch_bounds__(64 * WAVES, 2) void kv4_weight_rows_kernel(Kv4Atten
 #pragma unroll
           for (int t = TERMS - 1; t >= 0; --t) s[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(q[t][st], kf[j][st], s[j], 0, 0, 0);
       }
+      int last[4];                                     // this row sees the wave's tokens below it, counted from i
       if constexpr (masked) {
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const int last = w.ctx + query_of(a, m0 + r0 + 4 * g + r) + 1 - t0 - i;      // the row sees tokens below it
-#pragma unroll
-          for (int j = 0; j < 4; ++j) s[j][r] = 16 * j < last ? s[j][r] : -INFINITY;
-        }
+        for (int r = 0; r < 4; ++r) last[r] = w.ctx + query_of(a, m0 + r0 + 4 * g + r) + 1 - t0 - i;
       }
 #pragma unroll
       for (int j = 0; j < 4; ++j)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) sum[j] += __builtin_amdgcn_exp2f(fmaf(s[j][r], sc, -ls[r]));
+        for (int r = 0; r < 4; ++r) {
+          const float p = __builtin_amdgcn_exp2f(fmaf(s[j][r], sc, -ls[r]));
+          sum[j] += !masked || 16 * j < last[r] ? p : 0.f;      // (masked behind the exponential: a row whose log sum is NaN adds nothing where it does not look)
+        }
     }
   };
   int buf = 0;

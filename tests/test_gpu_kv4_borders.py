@@ -36,3 +36,52 @@ def test_bf16_rows_err_by_their_outputs_rounding(torch_mod, hkv, group, hd, lens
         err = np.abs(out.double().cpu().numpy().reshape(want.shape) - want)
         tol = 2.0**-8 * np.abs(want) + 1.01 * part + 1e-30
         assert (err <= tol).all(), (err / tol).max()
+
+
+def weights_of(cache, table, head, tokens):
+    """Bits of the weights of a request's first tokens."""
+    t = np.arange(tokens)
+    return cache.dev["weight"].cpu().numpy()[table[t // cache.size], head, t % cache.size].view(np.uint32)
+
+
+@pytest.mark.parametrize("bf16", [True, False])
+@pytest.mark.parametrize("hd,count", [(128, 6), (64, 8), (128, 9), (128, 40), (64, 70), (128, 150)])
+def test_weights_are_nan_only_where_a_nan_row_attends(torch_mod, bf16, hd, count):
+    """Of few and of many rows: a NaN query makes NaN the weights of the tokens up to its own, a NaN key those of its head, a NaN value none; all others keep the bits of a clean call."""
+    torch = torch_mod
+    hkv, group, size, ctx = 2, 2, 16, 80
+    dtype = torch.bfloat16 if bf16 else torch.float32
+    with Model(hkv, hd, bf16, group) as (B, h):
+        cache = R.Cache(B, 30, hkv, size, hd, 9)
+        tables = [cache.request(ctx + count, 15), cache.request(70, 15)]
+        s = cache.upload(B)
+        w0 = cache.dev["weight"].clone()
+        n = count + 4
+        q = torch.randn((n, 4 * hd), generator=torch.Generator().manual_seed(1)).to(dtype).cuda()
+        off, lens = torch.tensor([0, count, n], dtype=torch.int32, device="cuda"), torch.tensor([ctx, 60], dtype=torch.int32, device="cuda")
+        d_tab = torch.from_numpy(np.stack(tables)).cuda()
+
+        def go():
+            cache.dev["weight"].copy_(w0)
+            B.mace_kv4_attention(h, s, q, d_tab, lens, torch.empty_like(q), workspace(torch, B, h, 2, count, ctx), ctx, q_offsets=off, max_rows=count, add_weight=True)
+            torch.cuda.synchronize()
+            return [weights_of(cache, tables[0], hh, ctx + count) for hh in range(hkv)] + [weights_of(cache, tables[1], hh, 64) for hh in range(hkv)]
+
+        def same(got, but=()):
+            return all(np.array_equal(g, c) for k, (g, c) in enumerate(zip(got, clean)) if k not in but)
+
+        clean = go()
+        assert not any(np.isnan(c.view(np.float32)).any() for c in clean)
+        for row in (0, 1, count - 2, count - 1):
+            old = q[row, hd:2 * hd].clone()
+            q[row, hd:2 * hd] = float("nan")                  # query head 1, so kv head 0
+            got = go()
+            q[row, hd:2 * hd] = old
+            assert np.isnan(got[0].view(np.float32)[:ctx + row + 1]).all() and np.array_equal(got[0][ctx + row + 1:], clean[0][ctx + row + 1:]) and same(got, (0,))
+        at = (int(tables[0][83 // size]), 1, 83 % size)
+        for name, spread in (("v_scale", ()), ("k_scale", (1,))):
+            old = int(cache.dev[name][at][0])
+            cache.dev[name][at][0] = 255
+            got = go()
+            cache.dev[name][at][0] = old
+            assert same(got, spread) and all(np.isnan(got[k].view(np.float32)).all() for k in spread)
