@@ -421,9 +421,9 @@ int mace_kv4_gather(mace_handle_t h, const mace_kv4_cache_t *cache, const int32_
  *   lse           fp32 [n_rows, n_q_heads], optional: log sum exp of the row's scaled products
  *   add_weight    != 0: for every token that a row attends to, the probabilities summed over the rows of the request and the query heads of the kv head are added to
  *                 cache->weight.  The bits are a function of the inputs, except in blocks that requests of the call share: there the requests' sums arrive in any order
- * Rows of q and out that no request has are neither read nor written.  Tokens of blocks outside the cache are left out; a row without any token has out 0 and
- * lse -inf.  What lies behind a request's last token in its blocks is never used, whatever it holds.  A NaN in a key makes the rows that attend to it NaN, in a value
- * their 32 columns (a value whose probability is below 2^-126 of the row's largest may do so or not).  A row with a NaN in its query or in a key that it sees makes NaN
+ * Rows of q and out that no request has are neither read nor written.  Tokens of blocks outside the cache are left out; a row without any token, or all of whose
+ * products are -inf, has out 0 and lse -inf and adds to no weight.  What lies behind a request's last token in its blocks is never used, whatever it holds.  A NaN in a key
+ * makes the rows that attend to it NaN, in a value their 32 columns (a value whose probability is below 2^-126 of the row's largest may do so or not).  A row with a NaN in its query or in a key that it sees makes NaN
  * the weights of the tokens that it attends to, and no others.
  * Precision: codes and scales are exact; q is exact; in the product with V a probability carries 16 bits for bf16 models (off by at most 2^-16 of itself) and 24 bits
  * for fp32 ones; all sums are fp32; out is rounded once.  The sums are divided at the end: |v| times the number of tokens stays below 2^120.  workspace: mace_kv4_attention_workspace_bytes for the sizes of the call (other sizes can need more or less), 256-byte aligned,

@@ -936,7 +936,7 @@ __global__ __launch_bounds__(64 * WAVES) void kv4_weight_kernel(Kv4Attention a, 
       ls = ls * __builtin_amdgcn_exp2f(mn - base) + l2 * __builtin_amdgcn_exp2f(m2 - base);
       mn = top;
     }
-    if (threadIdx.x % 16 == 0) slse[row] = mn + log2f(ls);
+    if (threadIdx.x % 16 == 0) slse[row] = ls == 0.f ? INFINITY : mn + log2f(ls);      // (nothing is left of a row without a token, or all of whose products are -inf)
   }
   __syncthreads();
   float lse2[4];

@@ -85,3 +85,26 @@ def test_weights_are_nan_only_where_a_nan_row_attends(torch_mod, bf16, hd, count
             got = go()
             cache.dev[name][at][0] = old
             assert same(got, spread) and all(np.isnan(got[k].view(np.float32)).all() for k in spread)
+
+
+@pytest.mark.parametrize("bf16", [True, False])
+@pytest.mark.parametrize("hd,count", [(128, 2), (64, 6), (128, 40), (64, 70)])
+def test_products_that_are_all_minus_infinity(torch_mod, bf16, hd, count):
+    """Such a row is one without a token: out 0, lse -inf, and weights that keep their bits."""
+    torch = torch_mod
+    hkv, group, size, ctx = 1, 2, 16, 200
+    dtype = torch.bfloat16 if bf16 else torch.float32
+    with Model(hkv, hd, bf16, group) as (B, h):
+        cache = R.Cache(B, 20, hkv, size, hd, 4)
+        table = cache.request(ctx + count, 20)
+        cache.k[:] = 0xEE                                     # every key -4 steps (code 14)
+        s = cache.upload(B)
+        before = weights_of(cache, table, 0, ctx + count)
+        q = torch.full((count, group * hd), 3e38, dtype=dtype, device="cuda")
+        off, lens = torch.tensor([0, count], dtype=torch.int32, device="cuda"), torch.tensor([ctx], dtype=torch.int32, device="cuda")
+        out, lse = torch.full_like(q, 5.0), torch.full((count, group), 5.0, device="cuda")
+        B.mace_kv4_attention(h, s, q, torch.from_numpy(table[None]).cuda(), lens, out, workspace(torch, B, h, 1, count, ctx), ctx, q_offsets=off, max_rows=count, lse=lse, scale=1.0,
+                             add_weight=True)
+        torch.cuda.synchronize()
+        assert (out == 0).all() and torch.isneginf(lse).all()
+        assert np.array_equal(weights_of(cache, table, 0, ctx + count), before)
