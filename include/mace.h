@@ -441,7 +441,8 @@ int mace_kv4_attention(mace_handle_t h, const mace_kv4_cache_t *cache, const voi
  * token.  (Weights that are negative or NaN count as 0; tokens of blocks outside the cache rank last.)
  * Tokens that stay in front of new_lens remain where they are; the others that stay move into the places of those that go, in order: the i-th place from the front gets the
  * i-th token from the front.  Codes, scales, weight and position move; places from new_lens on keep what they held.  The order of tokens does not
- * matter to the attention: keys carry their rotary position.
+ * matter to the attention: keys carry their rotary position.  A place in a block outside the cache cannot be filled: the token that would move there, whatever its rank, is
+ * lost to the request (it stays where it was, behind new_lens), and new_lens counts the place, which the attention leaves out.
  *   context_lens  device int32 [n_req] or [n_req, n_kv_heads] (len_heads as above), at most max_context (larger ones are cut);  budgets  device int32 [n_req, n_kv_heads]
  *   seq_lens      device int32 [n_req]: tokens that the request has had in all, gone ones included; may be NULL where n_recent is 0
  *   new_lens      device int32 [n_req, n_kv_heads]; may be context_lens itself where len_heads = n_kv_heads

@@ -76,7 +76,7 @@ __device__ __forceinline__ int entry_of(const Lists &l, int m, int which) {
   for (int k = 1; k < NWAVES; ++k) w += m >= l.before[k][which];
   return (which ? l.moved : l.holes)[w * l.stride + m - l.before[w][which]];
 }
-// Moves the m-th displaced token to the m-th hole for m = first, first + step, .. below n, each by LANES lanes: a 16-byte piece of K or V a lane, and one of the small arrays in
+// Moves the m-th displaced token to the m-th hole (not where the hole lies in a block that does not exist) for m = first, first + step, .. below n, each by LANES lanes: a 16-byte piece of K or V a lane, and one of the small arrays in
 // each of the first four.  AT_ONCE of them are under way, loads before stores (one after the other, with a branch for each array, the moves of 8 x 8 heads x 6300 tokens of 128
 // took 60 us, now 47: 122 MB in pieces of 64 bytes).
 template <int HD>

@@ -108,3 +108,24 @@ def test_products_that_are_all_minus_infinity(torch_mod, bf16, hd, count):
         torch.cuda.synchronize()
         assert (out == 0).all() and torch.isneginf(lse).all()
         assert np.array_equal(weights_of(cache, table, 0, ctx + count), before)
+
+
+def test_eviction_into_a_missing_block(torch_mod):
+    """By hand: of tokens 0, 1 (no block), 2, 3 the two of largest weight stay, token 2 at place 0; token 3 would move to place 1, which there is none of, and stays behind the new length."""
+    torch = torch_mod
+    with Model(1, 64, True) as (B, h):
+        cache = R.Cache(B, 8, 1, 1, 64, 3)
+        table = cache.request(4, 4)
+        cache.weight[table] = np.float32([0.25, 0.75, 0.5, 1.0]).reshape(4, 1, 1)
+        names = ("k", "v", "k_scale", "v_scale", "weight", "position")
+        want = {n: getattr(cache, n).copy() for n in names}
+        for n in names:
+            want[n][table[0]] = want[n][table[2]]
+        s = cache.upload(B)
+        i32 = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")
+        new = i32([[-1]])
+        ws = torch.full((B.mace_kv4_evict_workspace_bytes(h, 1, 4),), 0xFF, dtype=torch.uint8, device="cuda")
+        B.mace_kv4_evict(h, s, i32([[table[0], 8, table[2], table[3]]]), i32([4]), None, i32([[2]]), new, ws, 4)
+        torch.cuda.synchronize()
+        assert new.tolist() == [[2]]
+        assert all(np.array_equal(cache.dev[n].cpu().numpy().view(np.uint8), x.view(np.uint8)) for n, x in want.items())
