@@ -36,11 +36,11 @@ __device__ __forceinline__ int wave_total(int v) {
 }
 
 // Larger is kept.  Weights (negative ones and NaN count as 0) below the newest, by position, below the first, by position.  A token in a block that
-// does not exist is the first to go.  0 is no token.
+// does not exist is the first to go.  0 is no token.  (Weights end at 0x7f800002, the newest at 0xbfffffff, and a sink in front of those is at least 0xc0000000.)
 __device__ __forceinline__ uint32_t key_from(float weight, int pos, bool ok, int n_sink, int newest) {
   const uint32_t p = (uint32_t)min(max(pos, 0), 0x3fffffff);
   uint32_t key = (weight > 0.f ? __float_as_uint(weight) : 0u) + 2u;
-  key = pos >= newest ? 0x80000002u + p : key;
+  key = pos >= newest ? 0x80000000u + p : key;
   key = pos < n_sink ? 0xfffffffeu - p : key;
   return ok ? key : 1u;
 }

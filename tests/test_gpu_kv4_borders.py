@@ -129,3 +129,20 @@ def test_eviction_into_a_missing_block(torch_mod):
         torch.cuda.synchronize()
         assert new.tolist() == [[2]]
         assert all(np.array_equal(cache.dev[n].cpu().numpy().view(np.uint8), x.view(np.uint8)) for n, x in want.items())
+
+
+@pytest.mark.parametrize("top", [100, 2**30 - 1])
+def test_sinks_rank_above_the_newest_up_to_the_last_position(torch_mod, top):
+    """Two tokens, the newest in front of a sink, one place: the sink takes it."""
+    torch = torch_mod
+    with Model(1, 64, True) as (B, h):
+        cache = R.Cache(B, 4, 1, 1, 64, 3)
+        table = cache.request(2, 2)
+        cache.position[table] = np.int32([top, top - 1]).reshape(2, 1, 1)
+        s = cache.upload(B)
+        i32 = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")
+        new = i32([[-1]])
+        ws = torch.full((B.mace_kv4_evict_workspace_bytes(h, 1, 2),), 0xFF, dtype=torch.uint8, device="cuda")
+        B.mace_kv4_evict(h, s, i32([list(table)]), i32([2]), i32([top + 1]), i32([[1]]), new, ws, 2, n_sink=top, n_recent=1)
+        torch.cuda.synchronize()
+        assert new.tolist() == [[1]] and int(cache.dev["position"][int(table[0])]) == top - 1
