@@ -304,7 +304,7 @@ __global__ __launch_bounds__(64 * WAVES, TERMS == 1 && HD == 64 ? 4 : 2) void kv
   const Rows w = rows_of<NR>(a, blockIdx.z, kvh, tile);
   if (w.m0 >= w.m1) return;
   const int end = w.ctx + query_of(a, w.m1 - 1) + 1;            // tokens that the last row sees
-  const int c0 = split * x.chunk, c1 = min(end, c0 + x.chunk);
+  const int c0 = split * x.chunk, c1 = split == x.nsplit - 1 ? end : min(end, c0 + x.chunk);      // (the last split takes a tail of up to a turn)
   if (c0 >= end && split > 0) return;                          // (the first one writes the rows that see nothing)
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i = lane & 15, g = lane >> 4, copy = i / NR;
   const int32_t *table = a.tables + (size_t)w.req * a.max_blocks;
@@ -1087,6 +1087,13 @@ __global__ __launch_bounds__(64 * WAVES, 2) void kv4_weight_rows_kernel(Kv4Atten
   }
 }
 
+// Splits of `chunk` tokens.  Bounds are powers of two as a rule, and the rows' own tokens come on top: a tail of up to a turn is the last split's where that leaves one split (no join:
+// 16 requests of 1024 tokens, 8 kv heads of 128, 14 us, and 17 with a split for the tail; 128 of 4096 122 and 162; 256 of 16384 749 and 797) or the chip is full; else a block of its
+// own costs nothing (4 of 2048 17.4, and 19 in the last split).
+int splits_for(long long blocks, int tokens, int chunk) {
+  const int n = std::max(1, cdiv(tokens - TURN, chunk));
+  return n == 1 || blocks * n >= 512 ? n : cdiv(tokens, chunk);
+}
 // Tokens of a block: 4096, less where that makes fewer blocks than two a CU, not below four turns of its waves (a second launch to join splits costs
 // more than it saves below that).  us at 256 / 512 / 1024 / 2048 / 4096 tokens, one row a request, 4 query heads a kv head: 4 requests of 400 - 1000 tokens, 8 kv heads of 128
 // 15.4 / 12.5 / 11.2 / 12.0 / 11.1; 16 of 1500 - 4000 22.5 / 22.1 / 19.9 / 22.3 / 26.9; 64 of 1500 - 4000 61 / 55 / 52 / 52 / 43; 1 of 60000 29.2 / 23.8 / 22.7 / 23.7 / 31.6.
@@ -1096,9 +1103,9 @@ __global__ __launch_bounds__(64 * WAVES, 2) void kv4_weight_rows_kernel(Kv4Atten
 // states of splits take no more than 540 MB.
 int chunk_tokens(int n_req, int tiles, int Hkv, int tokens) {
   const long long blocks = (long long)n_req * Hkv * tiles;
-  int chunk = blocks >= 1536 && tokens <= 16384 ? 16384 : 4096;
-  while (chunk > 4 * WAVES * TURN && blocks * cdiv(tokens, chunk) < 512) chunk /= 2;
-  while (chunk < tokens && blocks * cdiv(tokens, chunk) > (tiles > 1 ? 16384 : 65536)) chunk *= 2;
+  int chunk = blocks >= 1536 && splits_for(blocks, tokens, 16384) == 1 ? 16384 : 4096;
+  while (chunk > 4 * WAVES * TURN && blocks * splits_for(blocks, tokens, chunk) < 512) chunk /= 2;
+  while (chunk < tokens && blocks * splits_for(blocks, tokens, chunk) > (tiles > 1 ? 16384 : 65536)) chunk *= 2;
   return chunk;
 }
 // Rows of a kv head up to which the first kernel takes bf16 requests, tile by tile; us on it and on the kernel of many rows, 64 requests of 2000 tokens, 8 kv heads: 16 / 24 / 32 rows
@@ -1139,7 +1146,7 @@ Plan plan_of(int n_req, int max_rows, int max_context, int Hq, int Hkv, int hd, 
   p.tiles = cdiv(rows, p.tile_rows);
   p.workers = p.many ? workers_of(n_req, p.tiles, Hkv, tokens) : 0;
   p.chunk = p.workers ? tokens : p.many ? rows_chunk(n_req, p.tiles, Hkv, tokens) : chunk_tokens(n_req, p.tiles, Hkv, tokens);
-  p.nsplit = cdiv(tokens, p.chunk);
+  p.nsplit = p.many ? cdiv(tokens, p.chunk) : splits_for((long long)n_req * Hkv * p.tiles, tokens, p.chunk);
   p.rows = (size_t)n_req * max_rows * Hq;
   return p;
 }

@@ -3,7 +3,7 @@ import numpy as np
 import pytest
 
 import kv4_reference as R
-from test_gpu_kv4_attention import workspace
+from test_gpu_kv4_attention import run as attention_run, workspace
 from test_gpu_kv4_cache import Model
 
 pytestmark = pytest.mark.gpu
@@ -146,3 +146,12 @@ def test_sinks_rank_above_the_newest_up_to_the_last_position(torch_mod, top):
         B.mace_kv4_evict(h, s, i32([list(table)]), i32([2]), i32([top + 1]), i32([[1]]), new, ws, 2, n_sink=top, n_recent=1)
         torch.cuda.synchronize()
         assert new.tolist() == [[1]] and int(cache.dev["position"][int(table[0])]) == top - 1
+
+
+@pytest.mark.parametrize("bf16", [True, False])
+@pytest.mark.parametrize("hkv,group,hd,lens,counts", [
+    (1, 1, 128, [1024, 1000], [1, 1]), (2, 4, 64, [2048, 1025, 1024, 1023], [1, 1, 1, 1]), (1, 2, 128, [2047, 1026], [1, 1]), (1, 1, 64, [1024, 960], [16, 16]), (1, 1, 64, [1024], [64]),
+    (1, 1, 64, [1024], [65]), (1, 1, 64, [1086, 1088], [2, 1]), (8, 1, 64, [1024 * 32, 1024 * 31 + 5], [3, 1])])
+def test_the_last_split_takes_a_tail(torch_mod, bf16, hkv, group, hd, lens, counts):
+    """Splits of 1024 tokens: lengths with the rows' own tokens on both sides of what the last of them takes, 64 more (the last case: 32 splits in a full chip)."""
+    attention_run(torch_mod, bf16, hkv, group, hd, 16, lens, counts, seed=sum(lens))
