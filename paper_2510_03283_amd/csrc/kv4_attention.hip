@@ -1099,8 +1099,8 @@ int splits_for(long long blocks, int tokens, int chunk) {
 // 15.4 / 12.5 / 11.2 / 12.0 / 11.1; 16 of 1500 - 4000 22.5 / 22.1 / 19.9 / 22.3 / 26.9; 64 of 1500 - 4000 61 / 55 / 52 / 52 / 43; 1 of 60000 29.2 / 23.8 / 22.7 / 23.7 / 31.6.
 // Requests of up to 16384 tokens are not split where there are six blocks a CU without that, since a block's first loads and its end are worth two turns: at 4096 and whole 256 of 4000 - 16000 581 and
 // 496, 192 of them with 64-wide heads 288 and 255, 1024 2257 and 1762 (1024 blocks, 32 requests of 32 kv heads: 224 and 240; 300 of 1000 - 60000: 1667, and 2125 at 16384, where the last
-// long ones are alone).  More than 65536 blocks are never wanted, nor more than 16384 where a request has several tiles (one piece of 4096 fp32 rows at 16000: 4800 and 4400), so that the
-// states of splits take no more than 540 MB.
+// long ones are alone).  More than 65536 blocks are never wanted, nor more than 16384 where a request has several tiles (one piece of 4096 fp32 rows at 16000: 4800 and 4400), so that
+// there are no more than 2^20 states of rows: 537 MB of sums and 8 of maxima and sums of exponentials.
 int chunk_tokens(int n_req, int tiles, int Hkv, int tokens) {
   const long long blocks = (long long)n_req * Hkv * tiles;
   int chunk = blocks >= 1536 && splits_for(blocks, tokens, 16384) == 1 ? 16384 : 4096;

@@ -24,3 +24,22 @@ def test_bounds_that_are_powers_of_two_have_no_split_for_their_tail(recorder, n_
 def test_a_tail_in_an_idle_chip_is_a_split_of_its_own(recorder):
     launches, _ = attention(recorder, n_req=4, max_context=2048)
     assert launches[0]["grid"][1] == 3
+
+
+@pytest.mark.parametrize("bf16", [0, 1])
+@pytest.mark.parametrize("hkv,group,hd", [(8, 8, 128), (1, 1, 128), (32, 1, 64), (4, 4, 128), (64, 2, 64)])
+def test_states_of_splits_stay_within_a_million_rows(recorder, hkv, group, hd, bf16):
+    """2^20 states of HD sums, a maximum and a sum, and a log sum a row, each part rounded up to 256 bytes; only bounds that the call takes (else the size is 0)."""
+    most = 0
+    for n_req in (1, 7, 64, 1024, 8192, 65535):
+        for max_rows in (1, 2, 17, 300, 65535):
+            for max_context in (0, 1000, 16384, 131070, 1 << 20, 1 << 26):
+                need = recorder("attention", hkv=hkv, group=group, hd=hd, bf16=bf16, blocks=1000, n_req=n_req, max_rows=max_rows, max_context=max_context, tables=1)[3]
+                rows = n_req * max_rows * hkv * group
+                assert need <= (1 << 20) * (4 * hd + 8) + 12 * rows + 1024, (n_req, max_rows, max_context)
+                most = max(most, need)
+    assert most > 0
+
+
+def test_the_largest_states(recorder):
+    assert recorder("attention", hkv=8, group=8, hd=128, n_req=1024, max_rows=2, max_context=131070)[3] == (1 << 20) * 520 + (1 << 17) * 4
