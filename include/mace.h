@@ -366,7 +366,8 @@ int mace_token_logprobs_grad(mace_handle_t h, const void *logits, int32_t dtype,
  * mace_rotary_frequencies (host, pure): rot_dim / 2 frequencies in 64 bits,
  *   f_i = theta^(-2i/rot_dim),  inv_freq[i] = f_i (g_i + (1 - g_i) / factor),  g_i = clamp((original_len f_i / 2 pi - slow) / (fast - slow), 0, 1)
  * frequencies that turn at most `slow` times over the trained length original_len are divided by factor, those that turn at least
- * `fast` times stay.  original_len = 0: all are divided (g = 0, slow and fast unused); factor = 1: plain frequencies.  rot_dim even, 2..256.
+ * `fast` times stay.  original_len = 0: all are divided (g = 0, slow and fast unused); factor = 1: plain frequencies.  rot_dim even, 2..256.  A theta or
+ * factor so far below 1 that a frequency passes 2^19 (the most that mace_rotary takes) is refused; a refused call writes nothing.
  * mace_rotary turns the first rot_dim columns (even, <= head_dim) of n_heads heads in each of n rows,
  *   out[a] = magnitude (x[a] cos t - x[b] sin t),  out[b] = magnitude (x[b] cos t + x[a] sin t),  t = positions[r] inv_freq[i]
  * (a, b) = (i, i + rot_dim / 2), or (2 i, 2 i + 1) where interleaved != 0; columns of a head behind rot_dim are copied.  inverse != 0: t is

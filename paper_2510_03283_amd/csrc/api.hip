@@ -1008,11 +1008,14 @@ int mace_rotary_frequencies(int32_t rot_dim, double theta, double factor, int32_
   if (!(theta > 0.0) || !std::isfinite(theta) || !(factor > 0.0) || !std::isfinite(factor) || original_len < 0) return fail(MACE_INVALID_ARG, "mace_rotary_frequencies: theta and factor must be positive and finite, original_len at least 0");
   if (original_len > 0 && (!std::isfinite(slow) || !std::isfinite(fast) || !(slow < fast))) return fail(MACE_INVALID_ARG, "mace_rotary_frequencies: slow must be below fast");
   const double two_pi = 6.283185307179586476925;
+  double scaled[128];
   for (int32_t i = 0; i < rot_dim / 2; ++i) {
     const double f = std::pow(theta, -2.0 * i / rot_dim);
     const double keep = original_len > 0 ? std::min(std::max((original_len * f / two_pi - slow) / (fast - slow), 0.0), 1.0) : 0.0;
-    inv_freq[i] = f * (keep + (1.0 - keep) / factor);
+    scaled[i] = f * (keep + (1.0 - keep) / factor);
+    if (!(scaled[i] <= 524288.0)) return fail(MACE_INVALID_ARG, "mace_rotary_frequencies: theta and factor give a frequency above 2^19, which mace_rotary does not take");
   }
+  std::copy(scaled, scaled + rot_dim / 2, inv_freq);
   return MACE_OK;
 }
 
