@@ -489,7 +489,7 @@ def _head_rows(h, t, name: str, heads: int):
         raise MaceError(f"{name}: a matrix of {h.io_dtype} with adjacent columns, at least {heads} heads of {h.head_dim} of them, on cuda:{h.device} is wanted, "
                         f"got {t.dtype} {tuple(shape)} with strides {strides} on {t.device}")
     n = shape[0]
-    return t.data_ptr(), n, strides[0] if n > 1 else max(strides[0], shape[1])
+    return t.data_ptr(), n, strides[0] if n > 1 else heads * h.head_dim          # (one row has no stride)
 
 
 def mace_rotary(h, x, positions, inv_freq, out, n_heads: int, interleaved=False, magnitude: float = 1.0, inverse=False, stream=None):

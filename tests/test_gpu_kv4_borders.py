@@ -155,3 +155,32 @@ def test_sinks_rank_above_the_newest_up_to_the_last_position(torch_mod, top):
 def test_the_last_split_takes_a_tail(torch_mod, bf16, hkv, group, hd, lens, counts):
     """Splits of 1024 tokens: lengths with the rows' own tokens on both sides of what the last of them takes, 64 more (the last case: 32 splits in a full chip)."""
     attention_run(torch_mod, bf16, hkv, group, hd, 16, lens, counts, seed=sum(lens))
+
+
+@pytest.mark.parametrize("bf16", [True, False])
+def test_one_row_of_a_matrix_of_any_width(torch_mod, bf16):
+    """A single row has no stride: its matrix may be wider than the heads by any number of columns, in every operator that takes rows."""
+    torch = torch_mod
+    hkv, group, hd, size = 2, 2, 64, 16
+    dtype = torch.bfloat16 if bf16 else torch.float32
+    with Model(hkv, hd, bf16, group) as (B, h):
+        cache = R.Cache(B, 4, hkv, size, hd, 1)
+        table = cache.request(20, 2)
+        s = cache.upload(B)
+        i32 = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")
+        x = torch.randn((1, 4 * hd + 3), generator=torch.Generator().manual_seed(1)).to(dtype).cuda()
+        narrow, wide = (torch.full((1, 4 * hd + w), 5.0, dtype=dtype, device="cuda") for w in (0, 1))
+        freq = torch.from_numpy(B.mace_rotary_frequencies(hd, 1e4)).cuda()
+        slot = i32([int(table[1]) * size + 4])
+        for out, rows in ((narrow, x[:, :4 * hd].contiguous()), (wide, x)):
+            B.mace_rotary(h, rows, i32([20]), freq, out, 4)
+            B.mace_kv4_append(h, s, rows, rows, slot, i32([20]))
+            kept = [cache.dev[n].clone() for n in ("k", "v", "k_scale", "v_scale")]
+            turned = out.clone()
+            B.mace_kv4_attention(h, s, rows, i32([list(table)]), i32([20]), out, workspace(torch, B, h, 1, 1, 20), 20)
+            torch.cuda.synchronize()
+            if out is narrow:
+                first = kept, turned, out.clone()
+            else:
+                assert all(torch.equal(a, b) for a, b in zip(kept, first[0]))
+                assert torch.equal(turned[:, :-1], first[1]) and torch.equal(out[:, :-1], first[2]) and (out[:, -1] == 5).all()
