@@ -5,6 +5,7 @@ import pytest
 import kv4_reference as R
 from test_gpu_kv4_attention import run as attention_run, workspace
 from test_gpu_kv4_cache import Model
+from test_gpu_kv4_evict import expected as evicted, workspace as evict_workspace
 
 pytestmark = pytest.mark.gpu
 
@@ -184,3 +185,40 @@ def test_one_row_of_a_matrix_of_any_width(torch_mod, bf16):
             else:
                 assert all(torch.equal(a, b) for a, b in zip(kept, first[0]))
                 assert torch.equal(turned[:, :-1], first[1]) and torch.equal(out[:, :-1], first[2]) and (out[:, -1] == 5).all()
+
+
+@pytest.mark.parametrize("hd,bound,tokens,moves", [
+    (64, 8192, [8192, 8191], [600, 513]), (128, 8193, [8193, 8193, 8192], [511, 512, 513]), (64, 9000, [9000, 9000], [513, 512]), (128, 9000, [8900], [4000]),
+    (64, 32768, [32768, 32767], [512, 513]), (128, 32769, [32769, 32768], [513, 512]), (64, 32769, [5], [2])])
+def test_evictions_at_the_limits_of_their_kernels(torch_mod, hd, bound, tokens, moves):
+    """Bounds up to 8192 move everything in the selecting block, longer ones up to 512 tokens a head there and more in a launch of their own; up to 32768 keys stay in LDS.  Exactly
+    `moves` tokens of head 0 are displaced, fewer of head 1."""
+    torch, hkv, size = torch_mod, 2, 16
+    r = np.random.default_rng(bound + hd)
+    with Model(hkv, hd, True) as (B, h):
+        cache = R.Cache(B, sum(-(-t // size) for t in tokens) + 1, hkv, size, hd, 1)
+        width = -(-bound // size)
+        tables, budgets = [cache.request(t, width) for t in tokens], []
+        for table, n, m in zip(tables, tokens, moves):
+            keep = n - max(m, n // 3) if n > 5 else 3
+            budgets.append([keep] * hkv)
+            for head, k in ((0, m), (1, m // 2)):
+                w = r.random(n).astype(np.float32) / 4 + 1       # of those behind the new length only k stay, in the places of k in front of it
+                w[keep:] /= 8
+                w[r.choice(keep, k, replace=False)] /= 16
+                w[keep + r.choice(n - keep, k, replace=False)] += 2
+                t = np.arange(n)
+                cache.weight[table[t // size], head, t % size] = w
+        s = cache.upload(B)
+        i32 = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")
+        new = i32([[-1] * hkv] * len(tokens))
+        B.mace_kv4_evict(h, s, torch.from_numpy(np.stack(tables)).cuda(), i32(tokens), None, i32(budgets), new, evict_workspace(torch, B, h, len(tokens), bound), bound)
+        torch.cuda.synchronize()
+        want, lens = evicted(cache, tables, [[t] * hkv for t in tokens], budgets, tokens, 0, 0)
+        assert np.array_equal(new.cpu().numpy(), lens)
+        for table, m, (keep, _) in zip(tables, moves, budgets):
+            t = np.arange(keep)
+            at = (table[t // size], 0, t % size)
+            assert (want["position"][at] != cache.position[at]).sum() == m
+        for name, x in want.items():
+            assert np.array_equal(cache.dev[name].cpu().numpy().view(np.uint8), x.view(np.uint8)), name
