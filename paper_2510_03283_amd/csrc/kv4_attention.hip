@@ -55,6 +55,30 @@ __device__ __forceinline__ Rows rows_of(const Kv4Attention &a, int req, int kvh,
   return w;
 }
 
+// bf16 terms of a probability for rows of so many terms.
+constexpr int p_terms(int terms) { return terms == 1 ? 2 : terms; }
+// Eight numbers as MFMA operand in TERMS bf16 terms: the upper 8 bits of each (cut off: rounded up, the largest numbers would be infinite), of what is left, ..; the last term
+// is rounded to nearest.
+template <int TERMS>
+__device__ __forceinline__ void split8(float (&f)[8], bf16x8_t (&out)[TERMS]) {
+#pragma unroll
+  for (int t = 0; t < TERMS; ++t) {
+    uint32_t r[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if (t + 1 < TERMS) {
+        const uint32_t x = __float_as_uint(f[2 * e]), y = __float_as_uint(f[2 * e + 1]);
+        r[e] = __builtin_amdgcn_perm(y, x, 0x07060302u);     // the upper halves of both
+        f[2 * e] -= __uint_as_float(x & 0xffff0000u);
+        f[2 * e + 1] -= __uint_as_float(y & 0xffff0000u);
+      } else {
+        r[e] = cvt_pk_bf16(f[2 * e], f[2 * e + 1]);
+      }
+    }
+    out[t] = __builtin_bit_cast(bf16x8_t, make_uint4(r[0], r[1], r[2], r[3]));
+  }
+}
+
 // Q as MFMA operand: lane (i, g) holds row m (the last one again behind it), elements g HD / 4 + 8 s .. + 7 of step s, in TERMS bf16 terms; negated
 // where the scale is negative, so that the products' scale is not.
 template <int HD, int TERMS>
@@ -70,16 +94,12 @@ __device__ __forceinline__ void load_q(const Kv4Attention &a, const Rows &w, int
     } else {
       const float4 u = *(const float4 *)((const float *)a.q + o + 8 * s), v = *((const float4 *)((const float *)a.q + o + 8 * s) + 1);
       float f[8] = {u.x, u.y, u.z, u.w, v.x, v.y, v.z, v.w};
+      bf16x8_t y[TERMS];
+      split8<TERMS>(f, y);
 #pragma unroll
       for (int t = 0; t < TERMS; ++t) {
-        uint32_t r[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          r[e] = cvt_pk_bf16(f[2 * e], f[2 * e + 1]);
-          f[2 * e] -= __uint_as_float(r[e] << 16);
-          f[2 * e + 1] -= __uint_as_float(r[e] & 0xffff0000u);
-        }
-        q[t][s] = __builtin_bit_cast(bf16x8_t, make_uint4(r[0] ^ flip, r[1] ^ flip, r[2] ^ flip, r[3] ^ flip));
+        const uint4 r = __builtin_bit_cast(uint4, y[t]);
+        q[t][s] = __builtin_bit_cast(bf16x8_t, make_uint4(r.x ^ flip, r.y ^ flip, r.z ^ flip, r.w ^ flip));
       }
     }
   }
@@ -250,29 +270,6 @@ template <int HD>
 __device__ __forceinline__ float v_scale_of(const Turn<HD> &u, int j, int r, int gr) {
   if constexpr (HD == 128) return kv4::scale_value((u.vs[j][r] >> (8 * gr)) & 255u);
   else return kv4::scale_value((u.vs[j][r >> 1] >> (16 * (r & 1) + 8 * gr)) & 255u);
-}
-
-// bf16 terms of a probability for rows of so many terms.
-constexpr int p_terms(int terms) { return terms == 1 ? 2 : terms; }
-// Eight numbers as MFMA operand in TERMS bf16 terms: the upper 8 bits of each, of what is left, ..; the last term is rounded to nearest.
-template <int TERMS>
-__device__ __forceinline__ void split8(float (&f)[8], bf16x8_t (&out)[TERMS]) {
-#pragma unroll
-  for (int t = 0; t < TERMS; ++t) {
-    uint32_t r[4];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      if (t + 1 < TERMS) {
-        const uint32_t x = __float_as_uint(f[2 * e]), y = __float_as_uint(f[2 * e + 1]);
-        r[e] = __builtin_amdgcn_perm(y, x, 0x07060302u);     // the upper halves of both
-        f[2 * e] -= __uint_as_float(x & 0xffff0000u);
-        f[2 * e + 1] -= __uint_as_float(y & 0xffff0000u);
-      } else {
-        r[e] = cvt_pk_bf16(f[2 * e], f[2 * e + 1]);
-      }
-    }
-    out[t] = __builtin_bit_cast(bf16x8_t, make_uint4(r[0], r[1], r[2], r[3]));
-  }
 }
 
 // Where a call's workspace lies: partial sums [rows, splits, HD] and (maximum, sum) [rows, splits] of the splits, and log2 sum exp2 [rows] of rows that are done.

@@ -222,3 +222,28 @@ def test_evictions_at_the_limits_of_their_kernels(torch_mod, hd, bound, tokens, 
             assert (want["position"][at] != cache.position[at]).sum() == m
         for name, x in want.items():
             assert np.array_equal(cache.dev[name].cpu().numpy().view(np.uint8), x.view(np.uint8)), name
+
+
+@pytest.mark.parametrize("hd,count", [(128, 1), (64, 8), (128, 30)])
+def test_the_largest_fp32_queries_stay_finite(torch_mod, hd, count):
+    """Between the largest bf16 number and the largest fp32 one, against keys that are 0 there: as with 0 in their place, bit for bit."""
+    torch = torch_mod
+    hkv, group, size, ctx = 1, 2, 16, 100
+    with Model(hkv, hd, False, group) as (B, h):
+        cache = R.Cache(B, 20, hkv, size, hd, 4)
+        table = cache.request(ctx + count, 20)
+        cache.k[..., 3] &= 0xF0                               # element 6 of every key
+        s = cache.upload(B)
+        w0 = cache.dev["weight"].clone()
+        q = torch.randn((count, group * hd), generator=torch.Generator().manual_seed(1)).cuda()
+        off, lens = torch.tensor([0, count], dtype=torch.int32, device="cuda"), torch.tensor([ctx], dtype=torch.int32, device="cuda")
+        got = []
+        for x in (0.0, 3.4e38, -3.4028234663852886e38):
+            q[:, 6::hd] = x
+            cache.dev["weight"].copy_(w0)
+            out = torch.empty_like(q)
+            B.mace_kv4_attention(h, s, q, torch.from_numpy(table[None]).cuda(), lens, out, workspace(torch, B, h, 1, count, ctx), ctx, q_offsets=off, max_rows=count, add_weight=True)
+            torch.cuda.synchronize()
+            got.append((out.view(torch.int32).clone(), weights_of(cache, table, 0, ctx + count)))
+        assert torch.isfinite(got[0][0].view(torch.float32)).all()
+        assert all(torch.equal(g[0], got[0][0]) and np.array_equal(g[1], got[0][1]) for g in got[1:])
