@@ -418,7 +418,7 @@ int mace_kv4_gather(mace_handle_t h, const mace_kv4_cache_t *cache, const int32_
  *   context_lens  device int32 [n_req] (len_heads = 1) or [n_req, n_kv_heads] (len_heads = n_kv_heads)
  *   max_context, max_rows  bounds of context_lens and of a request's rows; the launches and the workspace go by them alone, so a captured call may be replayed with
  *                 other lengths, tables and offsets.  Values beyond them, negative ones and ones that the tables have no room for are cut to what fits
- *   scale         of the products q . k (usually head_dim^-1/2)
+ *   scale         of the products q . k (usually head_dim^-1/2), of magnitude up to 2^126
  *   lse           fp32 [n_rows, n_q_heads], optional: log sum exp of the row's scaled products
  *   add_weight    != 0: for every token that a row attends to, the probabilities summed over the rows of the request and the query heads of the kv head are added to
  *                 cache->weight.  The bits are a function of the inputs, except in blocks that requests of the call share: there the requests' sums arrive in any order

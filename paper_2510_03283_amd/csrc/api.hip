@@ -1134,7 +1134,7 @@ int mace_kv4_attention(mace_handle_t h, const mace_kv4_cache_t *cache, const voi
   if (n_req > 0 && n_rows > 0 && (!q || !block_tables || !context_lens || !out)) return fail(MACE_INVALID_ARG, "mace_kv4_attention: bad argument");
   if (!q_offsets && (max_rows != 1 || n_rows != n_req)) return fail(MACE_INVALID_ARG, "mace_kv4_attention: without q_offsets every request has one row");
   if (len_heads != 1 && len_heads != D.Hkv) return fail(MACE_BAD_SHAPE, "mace_kv4_attention: len_heads must be 1 or n_kv_heads");
-  if (!std::isfinite(scale)) return fail(MACE_INVALID_ARG, "mace_kv4_attention: scale must be finite");
+  if (!(std::fabs(scale) <= 0x1p126f)) return fail(MACE_INVALID_ARG, "mace_kv4_attention: scale must be of magnitude up to 2^126");
   if (add_weight && !c.weight) return fail(MACE_INVALID_ARG, "mace_kv4_attention: the cache has no weights to add to");
   const int64_t cols = (int64_t)D.Hq * D.hd;
   const int step = D.bf ? 8 : 4;

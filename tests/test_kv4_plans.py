@@ -1,7 +1,7 @@
 """What the operators on the 4-bit cache launch and how much workspace they take, by the bounds of a call, on a machine without a GPU."""
 import pytest
 
-from test_kv4_host import OK, recorder  # noqa: F401  (the fixture)
+from test_kv4_host import INVALID, OK, recorder  # noqa: F401  (the fixture)
 
 
 def attention(recorder, **opts):
@@ -43,3 +43,8 @@ def test_states_of_splits_stay_within_a_million_rows(recorder, hkv, group, hd, b
 
 def test_the_largest_states(recorder):
     assert recorder("attention", hkv=8, group=8, hd=128, n_req=1024, max_rows=2, max_context=131070)[3] == (1 << 20) * 520 + (1 << 17) * 4
+
+
+@pytest.mark.parametrize("scale,status", [(2.0**126, OK), (-(2.0**126), OK), (2.0**126 * (1 + 2.0**-23), INVALID), (3e38, INVALID), (-3e38, INVALID), ("-inf", INVALID)])
+def test_scales_whose_exponents_of_two_overflow_are_refused(recorder, scale, status):
+    assert recorder("attention", scale=scale)[0] == status
