@@ -375,7 +375,7 @@ int mace_token_logprobs_grad(mace_handle_t h, const void *logits, int32_t dtype,
  *   x, out     device io_dtype, n rows of n_heads * head_dim columns (queries and keys beside each other: n_heads = Hq + Hkv) that lie
  *              ld_x, ld_out elements apart; columns behind them are neither read nor written.  Aligned to their elements (16-byte aligned rows and
  *              rot_dim / 2 a multiple of 16 bytes run fastest).  out may be x (same stride); else they do not overlap, judged from first to last element
- *   positions  device int32 [n], any value;  inv_freq  device fp64 [rot_dim / 2], any finite values of magnitude up to 2^19;  magnitude finite;  n_heads 1..4096
+ *   positions  device int32 [n], any value;  inv_freq  device fp64 [rot_dim / 2], any finite values of magnitude up to 2^19;  magnitude finite in fp32;  n_heads 1..4096
  * No workspace; one launch (beyond 2^23 rows perhaps several).  The device of mace_create must be current (MACE_INVALID_ARG otherwise; so for the calls below). */
 int mace_rotary_frequencies(int32_t rot_dim, double theta, double factor, int32_t original_len, double slow, double fast, double *inv_freq);
 int mace_rotary(mace_handle_t h, const void *x, int64_t ld_x, const int32_t *positions, const double *inv_freq, int32_t rot_dim, int32_t interleaved,

@@ -1029,7 +1029,7 @@ int mace_rotary(mace_handle_t h, const void *x, int64_t ld_x, const int32_t *pos
   if (n_heads < 1 || n_heads > 4096) return fail(MACE_BAD_SHAPE, "mace_rotary: n_heads must be in 1..4096");
   const int64_t cols = (int64_t)n_heads * D.hd;
   if (ld_x < cols || ld_out < cols || ld_x > INT32_MAX || ld_out > INT32_MAX) return fail(MACE_BAD_SHAPE, "mace_rotary: a row stride must be at least n_heads * head_dim and below 2^31");
-  if (!std::isfinite(magnitude)) return fail(MACE_INVALID_ARG, "mace_rotary: magnitude must be finite");
+  if (!std::isfinite((float)magnitude)) return fail(MACE_INVALID_ARG, "mace_rotary: magnitude must be finite in fp32");
   const size_t es = D.bf ? 2 : 4;
   if (misaligned({x, out}, es) || misaligned({positions}, 4) || misaligned({inv_freq}, 8)) return fail(MACE_INVALID_ARG, "mace_rotary: pointer not aligned to its elements");
   if (n == 0) return MACE_OK;

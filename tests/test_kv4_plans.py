@@ -48,3 +48,8 @@ def test_the_largest_states(recorder):
 @pytest.mark.parametrize("scale,status", [(2.0**126, OK), (-(2.0**126), OK), (2.0**126 * (1 + 2.0**-23), INVALID), (3e38, INVALID), (-3e38, INVALID), ("-inf", INVALID)])
 def test_scales_whose_exponents_of_two_overflow_are_refused(recorder, scale, status):
     assert recorder("attention", scale=scale)[0] == status
+
+
+@pytest.mark.parametrize("magnitude,status", [(3.4028234e38, OK), (3.5e38, INVALID), (-1e300, INVALID), ("nan", INVALID)])
+def test_rotary_magnitudes_that_are_infinite_in_fp32_are_refused(recorder, magnitude, status):
+    assert recorder("rotary", magnitude=magnitude)[0] == status
