@@ -399,7 +399,8 @@ typedef struct {
  * the cache.  slot_mapping: device int32 [n] (slot_heads = 1), or [n, n_kv_heads] (slot_heads = n_kv_heads) where the heads of a row lie at different places, as behind
  * an eviction to budgets of their own.  -1 or slots out of range are skipped; two rows of a call do not share a slot of a head (what it then holds is unspecified).
  * A group of 32 with largest magnitude M takes the scale 2^e, e = floor(log2 M) - 2, plus 1 where M > 7 * 2^e, within -124..125, so that no
- * value is off by more than half of its own step; values go to the nearest, ties to the even code.  A group with a NaN or an infinity becomes NaN.
+ * value is off by more than half of its own step (but magnitudes above 7 * 2^125 become 6 * 2^125, the largest); values go to the nearest, ties to the even code.  A group
+ * with a NaN or an infinity becomes NaN.
  * weight (if the cache has it) becomes 0, position (if it has it) positions[r], device int32 [n], in 0..2^30 - 1. */
 int mace_kv4_append(mace_handle_t h, const mace_kv4_cache_t *cache, const void *k_new, int64_t ld_k, const void *v_new, int64_t ld_v,
                     const int32_t *slot_mapping, int32_t slot_heads, const int32_t *positions, int32_t n, void *stream);
@@ -417,15 +418,18 @@ int mace_kv4_gather(mace_handle_t h, const mace_kv4_cache_t *cache, const int32_
  *   block_tables  device int32 [n_req, max_blocks_per_req]
  *   context_lens  device int32 [n_req] (len_heads = 1) or [n_req, n_kv_heads] (len_heads = n_kv_heads)
  *   max_context, max_rows  bounds of context_lens and of a request's rows; the launches and the workspace go by them alone, so a captured call may be replayed with
- *                 other lengths, tables and offsets.  Values beyond them, negative ones and ones that the tables have no room for are cut to what fits
+ *                 other lengths, tables and offsets.  Values beyond them, negative ones and ones that the tables have no room for are cut to what fits.  Offsets do not
+ *                 descend (a row that two requests have holds either's result).  Splits follow max_context: requests far shorter than it run on fewer thread blocks, and
+ *                 add_weight launches blocks for max_context tokens, of which most then return, so several captured calls of different bounds serve mixed lengths best
  *   scale         of the products q . k (usually head_dim^-1/2), of magnitude up to 2^126
  *   lse           fp32 [n_rows, n_q_heads], optional: log sum exp of the row's scaled products
  *   add_weight    != 0: for every token that a row attends to, the probabilities summed over the rows of the request and the query heads of the kv head are added to
- *                 cache->weight.  The bits are a function of the inputs, except in blocks that requests of the call share: there the requests' sums arrive in any order
+ *                 cache->weight.  The bits are a function of the inputs, except in blocks that requests of the call share, or that a request's table has twice: there
+ *                 the sums arrive in any order
  * Rows of q and out that no request has are neither read nor written.  Tokens of blocks outside the cache are left out; a row without any token, or all of whose
  * products are -inf, has out 0 and lse -inf and adds to no weight.  What lies behind a request's last token in its blocks is never used, whatever it holds.  A NaN in a key
- * makes the rows that attend to it NaN, in a value their 32 columns (a value whose probability is below 2^-126 of the row's largest may do so or not).  A row with a NaN in its query or in a key that it sees makes NaN
- * the weights of the tokens that it attends to, and no others.
+ * makes the rows that attend to it NaN, in a value their 32 columns (a value whose probability is below 2^-126 of the row's largest may do so or not).  A row with a NaN in
+ * its query or in a key that it sees makes NaN the weights of the tokens that it attends to, and no others.
  * Precision: codes and scales are exact; q is exact; in the product with V a probability carries 16 bits for bf16 models (off by at most 2^-16 of itself) and 24 bits
  * for fp32 ones; all sums are fp32; out is rounded once.  The sums are divided at the end: |v| times the number of tokens stays below 2^120.  workspace: mace_kv4_attention_workspace_bytes for the sizes of the call (other sizes can need more or less), 256-byte aligned,
  * nothing of it read before it is written.  Outputs and workspace overlap neither an input nor each other, judged from first to last element.

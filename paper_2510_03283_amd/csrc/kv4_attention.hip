@@ -9,12 +9,12 @@
 // which is the order in which a transposing LDS read hands out 16 tokens of a channel of V.  K: a lane's elements (32 of a 128-wide head, 16 of a 64-wide one)
 // lie in one group, so its scale goes into the conversion to bf16.  V: the scale belongs to a token, which is the reduction index, so it goes into P, once
 // for every 32 channels.  Both conversions are exact; P enters as two bf16 terms for bf16 rows (16 bits: at most 2^-16 of each term) and as three
-// (24 bits) for fp32 rows, as q does.  Sums, maxima and the output before its rounding are fp32.  (One term, 2^-8 of a probability, is faster - 490 us against 515 for the
-// 128 requests below, 367 against 452 for 16 pieces of 256 rows behind 4000 tokens - but of values of either sign its error is two thirds of the output's own rounding,
+// (24 bits) for fp32 rows, as q does.  Sums, maxima and the output before its rounding are fp32.  (One term, 2^-8 of a probability, is faster - 477 us against 503 for the
+// 128 requests below, 407 against 505 for 16 pieces of 256 rows behind 4000 tokens - but of values of either sign its error is three quarters of the output's own rounding,
 // 2.1e-3 of the norm against 1.66e-3; two terms leave 1e-4 of difference to probabilities in fp32.)
 //
-// Few rows: the bytes of the cache bound it, so tokens are split over waves and blocks (128 requests of 2048 to 8192 tokens, 32 heads of 128: 479 us, 6.2 TB/s; one of 131001, 8 kv heads: 29 us
-// and 5 for the join, 4.9 TB/s).  A short batch is a chain of loads, table - codes - products (32 requests of 256 to 2048 tokens, 8 kv heads of 64: 12 us).  Many rows: the instructions, below.
+// Few rows: the bytes of the cache bound it, so tokens are split over waves and blocks (128 requests of 2048 to 8192 tokens, 32 heads of 128: 503 us, 5.9 TB/s; one of 131001, 8 kv heads: 30 us
+// and 4 for the join, 4.7 TB/s).  A short batch is a chain of loads, table - codes - products (32 requests of 256 to 2048 tokens, 8 kv heads of 64: 12 us).  Many rows: the instructions, below.
 #include "kernels.h"
 #include "kv4.h"
 
@@ -242,7 +242,7 @@ __device__ __forceinline__ void mask_scores(f32x4_t (&s)[4], int last, uint64_t 
 }
 // Soft-max of a row, whose tokens are spread over four lanes: probabilities are 2^(sc s - top), and `top` follows the largest product only when one is more than `lag`
 // above it.  lag = MANY_LAG, where many rows make the instructions count: most turns need neither an exchange between lanes nor a rescaling (a piece of 4096 rows, 32 heads
-// and 8 kv heads of 128, behind 4096 tokens 483 -> 457 us when P had one term).  The relative error of a probability does not depend on it.
+// and 8 kv heads of 128, behind 4096 tokens 680 -> 652 us).  The relative error of a probability does not depend on it.
 constexpr float MANY_LAG = 8.f;
 struct Softmax {
   float top = -INFINITY, minus = 0.f, l = 0.f;        // minus: -top, 0 as long as the row has seen nothing; l: this lane's part of the sum
@@ -444,15 +444,15 @@ __global__ __launch_bounds__(64 * WAVES, TERMS == 1 && HD == 64 ? 4 : 2) void kv
 // and are decoded by every wave (a quarter of the bytes that decoded ones would be read in), the value's are decoded with their scale first and lie there as bf16, token by token,
 // so that P needs no scaling and a transposing read of 4 tokens x 16 channels hands out V^T.  A value group that is NaN counts as 0 there and is noted beside it: only the
 // rows that see the token become NaN.  A turn's codes are asked for two turns ahead, put into LDS one ahead, their
-// blocks looked up three ahead.  A piece of 4096 rows, 32 heads and 8 kv heads of 128, behind 4096 tokens takes 440 - 457 us, 0.90 - 0.94 PFLOP/s: the matrix pipes are busy for 39 % of the
-// cycles, vector instructions (exponentials, roundings, maxima, decoding, the issue of the products) take 65 %.
+// blocks looked up three ahead.  A piece of 4096 rows, 32 heads and 8 kv heads of 128, behind 4096 tokens takes 656 us, 0.63 PFLOP/s (0.94 with the second term of P): the matrix pipes are
+// busy for 45 % of the cycles, vector instructions (exponentials, terms, maxima, decoding, the issue of the products) take 64 %.
 constexpr int ROW_TILES = 2, BLOCK_ROWS = WAVES * ROW_TILES * ROWS, LEAST_TURNS = 4, NEAR = 2;
 typedef __attribute__((ext_vector_type(4))) short s16x4_t;
 typedef __attribute__((address_space(3))) s16x4_t lds_s16x4_t;
 
 // The work of a kv head, the turns of all blocks of rows of all requests one after the other, is cut into equal shares, one a thread block, since lengths and rows are known on the device only and
-// differ (a grid of requests, blocks of rows and equal splits of the longest context leaves the chip half idle: 6 requests of 134 to 238 rows at 2500 to 6700 tokens, 8 kv heads of 128, with
-// weights 218 us, now 194; 64 of 5 to 60 rows at 500 to 6000 335, now 220).  A block of rows that is cut leaves states that
+// differ (a grid of requests, blocks of rows and equal splits of the longest context leaves the chip half idle: six requests of 134 to 238 rows at 2500 to 6700 tokens, 8 kv heads of 128, 209
+// us and by shares 167; 64 of 5 to 60 rows at 500 to 6000 435 and 277).  A block of rows that is cut leaves states that
 // kv4_rows_join_kernel joins; a cut NEAR turns or less from the rows' begin or end, the price of one, moves there.
 // (With workers = 0 the thread blocks are the splits of the blocks of rows, as few rows have them.)
 struct Shares {
@@ -1093,9 +1093,9 @@ int splits_for(long long blocks, int tokens, int chunk) {
 }
 // Tokens of a block: 4096, less where that makes fewer blocks than two a CU, not below four turns of its waves (a second launch to join splits costs
 // more than it saves below that).  us at 256 / 512 / 1024 / 2048 / 4096 tokens, one row a request, 4 query heads a kv head: 4 requests of 400 - 1000 tokens, 8 kv heads of 128
-// 15.4 / 12.5 / 11.2 / 12.0 / 11.1; 16 of 1500 - 4000 22.5 / 22.1 / 19.9 / 22.3 / 26.9; 64 of 1500 - 4000 61 / 55 / 52 / 52 / 43; 1 of 60000 29.2 / 23.8 / 22.7 / 23.7 / 31.6.
-// Requests of up to 16384 tokens are not split where there are six blocks a CU without that, since a block's first loads and its end are worth two turns: at 4096 and whole 256 of 4000 - 16000 581 and
-// 496, 192 of them with 64-wide heads 288 and 255, 1024 2257 and 1762 (1024 blocks, 32 requests of 32 kv heads: 224 and 240; 300 of 1000 - 60000: 1667, and 2125 at 16384, where the last
+// 14.6 / 12.6 / 11.2 / 11.5 / 12.0; 16 of 1500 - 4000 23.1 / 23.9 / 21.4 / 22.3 / 30.0; 64 of 1500 - 4000 69 / 61 / 59 / 58 / 51; 1 of 60000 29.8 / 25.8 / 24.2 / 24.5 / 33.9.
+// Requests of up to 16384 tokens are not split where there are six blocks a CU without that, since a block's first loads and its end are worth two turns: at 4096 and whole 256 of 4000 - 16000 640 and
+// 546, 192 of them with 64-wide heads 314 and 278, 1024 2334 and 1862 (1024 blocks, 32 requests of 32 kv heads: 248 and 259; 300 of 1000 - 60000: 1784, and 2177 at 16384, where the last
 // long ones are alone).  More than 65536 blocks are never wanted, nor more than 16384 where a request has several tiles (one piece of 4096 fp32 rows at 16000: 4800 and 4400), so that
 // there are no more than 2^20 states of rows: 537 MB of sums and 8 of maxima and sums of exponentials.
 int chunk_tokens(int n_req, int tiles, int Hkv, int tokens) {
@@ -1106,7 +1106,7 @@ int chunk_tokens(int n_req, int tiles, int Hkv, int tokens) {
   return chunk;
 }
 // Rows of a kv head up to which the first kernel takes bf16 requests, tile by tile; us on it and on the kernel of many rows, 64 requests of 2000 tokens, 8 kv heads: 16 / 24 / 32 rows
-// of 128-wide heads 44 and 72 / 72 and 68 / 73 and 69, 32 / 48 / 64 rows of 64-wide ones 41 and 56 / 60 and 69 / 77 and 70.
+// of 128-wide heads 48 and 84 / 87 and 80 / 85 and 80, 32 / 48 / 64 rows of 64-wide ones 47 and 64 / 66 and 85 / 89 and 84.
 int few_rows(int hd) { return hd == 128 ? 16 : 48; }
 // Splits of a block of rows: two thread blocks a CU, or splits of four turns.
 int rows_chunk(int n_req, int tiles, int Hkv, int tokens) {
@@ -1116,9 +1116,9 @@ int rows_chunk(int n_req, int tiles, int Hkv, int tokens) {
 }
 // Thread blocks of a kv head for shares, two a CU in all; 0: blocks of rows and their splits are the thread blocks, long ones first.  That is for many blocks of rows, for twice as many as run at once
 // that come from long pieces, whose blocks are alike, and for short work, where finding the shares costs more than they give; few rows a request, of any lengths, need shares.  us by
-// blocks and by shares, 8 kv heads of 128: a piece of 4096 rows behind 4096 tokens 439 and 483, three of 600 to 2000 rows 135 and 159; 96 requests of 5 to 60 rows at 500 to 6000 tokens 488
-// and 340, 120 of them 561 and 407 (16 of 256 rows at 4000 each, 32 heads: 377 and 398); one of 64 rows at 2000 22 and 34, 64 of 8 rows at 300 to 700 28 and 38, 32 of 5 to 30 rows
-// at 300 to 2000, 16 turns a share, 55 and 48, six of 37 to 256 rows at 1000 to 2000, 24 turns, 77 and 62.
+// blocks and by shares, 8 kv heads of 128: a piece of 4096 rows behind 4096 tokens 659 and 702, three of 600 to 2000 rows 173 and 196; 96 requests of 5 to 60 rows at 500 to 6000 tokens 635
+// and 477, 120 of them 727 and 522 (16 of 256 rows at 4000 each, 32 heads: 458 and 458); one of 64 rows at 2000 24 and 31, 64 of 8 rows at 300 to 700 30 and 41, 32 of 5 to 30 rows
+// at 300 to 2000, 16 turns a share, 67 and 56, six of 37 to 256 rows at 1000 to 2000, 24 turns, 93 and 70.
 constexpr int ENOUGH = 2000, ENOUGH_ALIKE = 1024, ALIKE = 16, SHORT = 14;
 int workers_of(int n_req, int tiles, int Hkv, int tokens) {
   const long long blocks = (long long)n_req * tiles, turns = blocks * cdiv(tokens, TURN);
